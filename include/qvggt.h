@@ -478,6 +478,55 @@ int qvggt_calib_loss_grad(const float *R, const float *V, const float *y_ref, co
 int qvggt_calib_descent_step(float *theta, const float *grad, int n, float lr, float floor, void *stream);
 
 /*
+ * A key/value cache held in 4 bits, in pages, and attention over it: what follows the qkv layer of a block that keeps the keys and values of earlier
+ * tokens or frames.  The quantizer is the one of the linear layer (Sec. 3.2: random signs, Hadamard rotation, symmetric 4-bit codes with a step per token), applied to
+ * every head of a token: with d channels, signs s, the orthonormal Sylvester-Hadamard matrix H of d channels,
+ *     z = (s * x) H,   step = bf16_rne(max_j |z_j| / 7),   code_j = rne(z_j / step) in [-7, 7],      and x is kept as   x^ = s * ((step * code) H).
+ * A row of zeros, or one whose step would lie below 2^-126, has step 0 and codes 0.
+ *
+ * Pages.  d = 64 or 128 channels; a page holds page_tokens tokens (a power of two, 16 .. 1024) of all `heads` key/value heads in
+ * qvggt_kv4_page_bytes(page_tokens, heads, d) = heads * page_tokens * (d + 4) bytes (0 for unsupported sizes); a pool of num_pages of them is one buffer, `cache`, of
+ * less than 2^31 tokens.  Slot number page * page_tokens + offset names a token's place.  Inside a page, head after head: the keys' codes
+ * (token after token, d / 2 bytes: channel 2 j in the low half of byte j, 2 j + 1 in the high half), the values' codes (blocks of 16 tokens, in each
+ * [4 groups of 4 tokens][16][d / 32][4 tokens] bytes, a byte being channels 2 p and 2 p + 1 of one token at [p / (d / 32)][p % (d / 32)]), the steps (4 bytes a token: bf16 of
+ * the key, then of the value).  Codes are kept as code + 8.
+ *
+ * Rotation by position.  rope: f32 [rope_rows, rope_dim], cosines in the first half of a row, sines in the second; positions: int32 [T], the row of every token (rows outside the
+ * table are taken as its first or last).  Of the first rope_dim channels, in consecutive groups of 2 * rope_pair, channel c turns with c + rope_pair:
+ *     (a, b) -> (a cos_p - b sin_p,  b cos_p + a sin_p),      p = (c / (2 rope_pair)) * rope_pair + c % rope_pair.
+ * rope_pair = rope_dim / 2 turns the halves of a head, 1 neighbouring channels, rope_dim / 4 each half of the channels by an angle of its own (rows and columns of an image).
+ * rope_dim a multiple of 16 and of 2 * rope_pair, at most d; rope_pair a power of two.  rope = NULL: no rotation, and positions, rope_rows, rope_dim and rope_pair are not looked at.
+ *
+ * qvggt_kv4_append:  keys (rotated) and values of T tokens into their slots.  K, V: bf16 or f32, token t at k_stride * t resp. v_stride * t elements, its heads one after
+ *   another (rows of a fused qkv product as they are); strides in elements, a multiple of 16 bytes, not negative.  signs: int8 [d] of +1/-1, or NULL for +1.  slots: int32 [T]; tokens with
+ *   a slot outside the pool, -1 for example, are left out.  Two tokens of one call must not have the same slot.
+ * qvggt_kv4_read:    what slots hold: K and V [T, heads, d] bf16 or f32, either may be NULL; zeros for slots outside the pool.
+ * qvggt_kv4_attention:  for every sequence b, its n = q_starts[b + 1] - q_starts[b] query tokens (rows q_starts[b] .. of Q) over its first len = kv_lens[b] keys and values, which lie
+ *   in the pages page_table[b, 0], page_table[b, 1], ...:
+ *     out[i, h, :] = sum_j softmax_j( scale * <rotated q[i, h], k^[j, h']> ) v^[j, h'],     h' = h / (q_heads / kv_heads),
+ *   j over the keys 0 .. len - n + i with causal = 1 (the queries are the sequence's last n tokens), 0 .. len - 1 with causal = 0.  A query that sees no key gives zeros.
+ *   Q: bf16 or f32 [T, q_heads, d], token t at q_stride * t elements.  q_heads a multiple of kv_heads.  signs as given to qvggt_kv4_append.  q_starts: int32 [seqs + 1], not falling;
+ *   kv_lens: int32 [seqs]; page_table: int32 [seqs, table_width].  max_q and max_kv: at least every n and len (they decide how the work is cut up; longer sequences are cut off at them),
+ *   max_kv <= table_width * page_tokens.  What lies in pages behind a sequence's end, and entries of page_table behind its last page, may be anything.  An entry in use that is no page of
+ *   the pool gives wrong results for its sequence, and nothing is read outside the pool.  seqs <= 65535.  out: bf16 [T, q_heads, d]; rows of no sequence are not written.
+ *   workspace: qvggt_kv4_attention_workspace_bytes of the same sizes, 16-byte aligned, NULL where that is 0.  Scores, weights and sums are fp32, queries and weights are rounded to fp16
+ *   (11 bits) for the products.  Sums in a fixed order: the same call gives the same bits.
+ * QVGGT_ERR_SHAPE for sizes outside these limits, QVGGT_ERR_ARG for a scale that is not finite or a causal other than 0 and 1.  int32 arrays and tables need 16-byte aligned pointers as
+ * everything else.
+ */
+size_t qvggt_kv4_page_bytes(int page_tokens, int heads, int d);
+int qvggt_kv4_append(const void *K, const void *V, int x_dtype, int T, long long k_stride, long long v_stride, int heads, int d, const float *rope, int rope_rows,
+                     int rope_dim, int rope_pair, const int32_t *positions, const int8_t *signs, const int32_t *slots, void *cache, int num_pages, int page_tokens,
+                     void *stream);
+int qvggt_kv4_read(const void *cache, int num_pages, int page_tokens, int heads, int d, const int8_t *signs, const int32_t *slots, int T, int out_dtype, void *K,
+                   void *V, void *stream);
+size_t qvggt_kv4_attention_workspace_bytes(int T, int seqs, int max_q, int max_kv, int q_heads, int kv_heads, int d);
+int qvggt_kv4_attention(const void *Q, int q_dtype, int T, long long q_stride, int q_heads, const float *rope, int rope_rows, int rope_dim, int rope_pair,
+                        const int32_t *positions, const int8_t *signs, float scale, int causal, const void *cache, int num_pages, int page_tokens, int kv_heads, int d,
+                        const int32_t *page_table, int table_width, const int32_t *q_starts, const int32_t *kv_lens, int seqs, int max_q, int max_kv, void *out,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Measurement helper (used by the benchmark, not by the path): a register-only loop of the matrix instruction that the GEMMs of
  * many tokens are built on, to state what the matrix pipes of this board sustain on codes of a normal distribution when nothing has
  * to be fed to them.  One launch runs 256 blocks x 4 waves x iters x 32 instructions; kind 0: v_mfma_i32_16x16x64_i8 (2 * 16 * 16 * 64

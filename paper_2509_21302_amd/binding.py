@@ -45,6 +45,7 @@ EXPORTS = [
     "qvggt_nfds_keep_lowest", "qvggt_nfds_kmeans_step",
     "qvggt_linear_e2m3_any", "qvggt_layer_workspace_bytes", "qvggt_layer_statistics", "qvggt_layer_codes",
     "qvggt_rotate_rows", "qvggt_calib_workspace_bytes", "qvggt_calib_loss_grad", "qvggt_calib_descent_step",
+    "qvggt_kv4_page_bytes", "qvggt_kv4_append", "qvggt_kv4_read", "qvggt_kv4_attention_workspace_bytes", "qvggt_kv4_attention",
 ]
 
 
@@ -192,6 +193,16 @@ def load_library() -> C.CDLL:
     lib.qvggt_calib_loss_grad.argtypes = [vp, vp, vp, vp, vp, vp, vp, i, i, i, i, vp, vp, vp, vp, vp, sz, vp]
     lib.qvggt_calib_descent_step.restype = i
     lib.qvggt_calib_descent_step.argtypes = [vp, vp, i, f, f, vp]
+    lib.qvggt_kv4_page_bytes.restype = sz
+    lib.qvggt_kv4_page_bytes.argtypes = [i, i, i]
+    lib.qvggt_kv4_append.restype = i
+    lib.qvggt_kv4_append.argtypes = [vp, vp, i, i, ll, ll, i, i, vp, i, i, i, vp, vp, vp, vp, i, i, vp]
+    lib.qvggt_kv4_read.restype = i
+    lib.qvggt_kv4_read.argtypes = [vp, i, i, i, i, vp, vp, i, i, vp, vp, vp]
+    lib.qvggt_kv4_attention_workspace_bytes.restype = sz
+    lib.qvggt_kv4_attention_workspace_bytes.argtypes = [i, i, i, i, i, i, i]
+    lib.qvggt_kv4_attention.restype = i
+    lib.qvggt_kv4_attention.argtypes = [vp, i, i, ll, i, vp, i, i, i, vp, vp, f, i, vp, i, i, i, i, vp, i, vp, vp, i, i, i, vp, vp, sz, vp]
     lib.qvggt_workspace_bytes.restype = sz
     lib.qvggt_workspace_bytes.argtypes = [i, i, i]
     lib.qvggt_pack_int4.restype = i
@@ -634,3 +645,88 @@ def qvggt_calib_loss_grad(R, V, y_ref, bias, c_hat, w_step, x_step, bits, loss, 
 def qvggt_calib_descent_step(theta, grad, lr, floor=1e-8, stream=None):
     _check(load_library().qvggt_calib_descent_step(_ptr(theta), _ptr(grad), theta.numel(), float(lr), float(floor), _stream(stream)),
            "qvggt_calib_descent_step")
+
+
+# ---- the 4-bit key/value cache
+def _heads_of(t, name):
+    """(device pointer, elements from token to token) of a [T, heads, d] tensor whose heads follow one another: a slice of a fused product's rows is one."""
+    if not t.is_cuda:
+        raise ValueError("qvggt takes device tensors only")
+    if t.dim() != 3 or t.numel() and (t.stride(2) != 1 or t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise ValueError(f"{name}: [tokens, heads, channels] with every token's heads one after another")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _whole(t, name, dtype, count):
+    """Device pointer of a contiguous tensor of `count` elements of a type (None -> NULL)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != count:
+        raise ValueError(f"{name}: {count} elements of {dtype}, not {t.numel()} of {t.dtype}")
+    return _ptr(t)
+
+
+def _rope_of(rope, positions, T):
+    """rope, rope_rows, rope_dim, positions as the entry points take them."""
+    if rope is None:
+        return None, 0, 0, None
+    if rope.dim() != 2 or positions is None:
+        raise ValueError("rope: [rows, rope_dim], with positions")
+    return _whole(rope, "rope", torch.float32, rope.numel()), rope.shape[0], rope.shape[1], _whole(positions, "positions", torch.int32, T)
+
+
+def _pool_of(cache, page_tokens, heads, d):
+    """(device pointer, pages) of a pool."""
+    size = qvggt_kv4_page_bytes(page_tokens, heads, d)
+    if size == 0:
+        raise QvggtError(ERR_SHAPE, "qvggt_kv4: page")
+    if cache.numel() % size or cache.element_size() != 1:
+        raise ValueError(f"cache: pages of {size} bytes")
+    return _ptr(cache), cache.numel() // size
+
+
+def qvggt_kv4_page_bytes(page_tokens: int, heads: int, d: int) -> int:
+    return int(load_library().qvggt_kv4_page_bytes(int(page_tokens), int(heads), int(d)))
+
+
+def qvggt_kv4_append(K, V, signs, slots, cache, page_tokens, rope=None, positions=None, rope_pair=0, stream=None):
+    T, heads, d = K.shape
+    if V.shape != K.shape or V.dtype != K.dtype:
+        raise ValueError("V: the shape and type of K")
+    k, k_stride = _heads_of(K, "K")
+    v, v_stride = _heads_of(V, "V")
+    table, rows, dim, at = _rope_of(rope, positions, T)
+    pool, pages = _pool_of(cache, page_tokens, heads, d)
+    _check(load_library().qvggt_kv4_append(k, v, _dtype_code(K), T, k_stride, v_stride, heads, d, table, rows, dim, int(rope_pair), at,
+                                           _whole(signs, "signs", torch.int8, d), _whole(slots, "slots", torch.int32, T), pool, pages, int(page_tokens),
+                                           _stream(stream)), "qvggt_kv4_append")
+
+
+def qvggt_kv4_read(cache, page_tokens, signs, slots, K, V, stream=None):
+    out = K if K is not None else V
+    T, heads, d = out.shape
+    if K is not None and V is not None and (V.shape != K.shape or V.dtype != K.dtype):
+        raise ValueError("V: the shape and type of K")
+    pool, pages = _pool_of(cache, page_tokens, heads, d)
+    _check(load_library().qvggt_kv4_read(pool, pages, int(page_tokens), heads, d, _whole(signs, "signs", torch.int8, d), _whole(slots, "slots", torch.int32, T), T,
+                                         _dtype_code(out), _ptr(K), _ptr(V), _stream(stream)), "qvggt_kv4_read")
+
+
+def qvggt_kv4_attention_workspace_bytes(T: int, seqs: int, max_q: int, max_kv: int, q_heads: int, kv_heads: int, d: int) -> int:
+    return int(load_library().qvggt_kv4_attention_workspace_bytes(int(T), int(seqs), int(max_q), int(max_kv), int(q_heads), int(kv_heads), int(d)))
+
+
+def qvggt_kv4_attention(Q, signs, scale, causal, cache, page_tokens, kv_heads, page_table, q_starts, kv_lens, max_q, max_kv, out, workspace, rope=None,
+                        positions=None, rope_pair=0, stream=None):
+    T, heads, d = Q.shape
+    at_q, q_stride = _heads_of(Q, "Q")
+    if out.shape != Q.shape or out.dtype != torch.bfloat16:
+        raise ValueError("out: bf16 of the shape of Q")
+    seqs, width = page_table.shape
+    table, rows, dim, at = _rope_of(rope, positions, T)
+    pool, pages = _pool_of(cache, page_tokens, kv_heads, d)
+    _check(load_library().qvggt_kv4_attention(at_q, _dtype_code(Q), T, q_stride, heads, table, rows, dim, int(rope_pair), at, _whole(signs, "signs", torch.int8, d),
+                                              float(scale), int(causal), pool, pages, int(page_tokens), int(kv_heads), d,
+                                              _whole(page_table, "page_table", torch.int32, seqs * width), width, _whole(q_starts, "q_starts", torch.int32, seqs + 1),
+                                              _whole(kv_lens, "kv_lens", torch.int32, seqs), seqs, int(max_q), int(max_kv), _ptr(out), _ptr(workspace),
+                                              0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)), "qvggt_kv4_attention")

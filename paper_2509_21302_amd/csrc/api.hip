@@ -1,6 +1,7 @@
 // C ABI of the qvggt library: argument validation on the host, then kernel launches on the
 // caller's stream.  Declarations and the meaning of every argument are in include/qvggt.h.
 #include "qvggt_common.h"
+#include "kv4.h"
 #include "../../include/qvggt.h"
 
 #include <atomic>
@@ -841,6 +842,90 @@ int qvggt_calib_descent_step(float *theta, const float *grad, int n, float lr, f
     if (!theta || !grad) return QVGGT_ERR_NULL;
     if (!aligned4(theta) || !aligned4(grad)) return QVGGT_ERR_ALIGN;
     return hip_status(qvggt::run_descent_step(theta, grad, n, lr, floor, static_cast<hipStream_t>(stream)));
+}
+
+// ---- the 4-bit key/value cache
+namespace {
+bool valid_rope(const float *table, int rows, int dim, int pair, int d)
+{
+    return table == nullptr || (rows >= 1 && dim >= 16 && dim <= d && dim % 16 == 0 && pair >= 1 && (pair & (pair - 1)) == 0 && dim % (2 * pair) == 0);
+}
+// pages whose tokens have int32 slot numbers
+bool valid_pages(int num_pages, int page_tokens, int heads, int d)
+{
+    return qvggt::kv4_valid_page(page_tokens) && qvggt::kv4_valid_head(d) && heads >= 1 && heads <= 65535 && num_pages >= 0 &&
+           (long long)num_pages * page_tokens < (1LL << 31);
+}
+qvggt::Kv4Pages pages_of(const void *cache, int num_pages, int page_tokens, int heads)
+{
+    return {static_cast<uint8_t *>(const_cast<void *>(cache)), num_pages, __builtin_ctz((unsigned)page_tokens), heads};
+}
+bool valid_rows(int T, int heads) { return T >= 0 && (long long)T * heads <= (1LL << 33); }
+bool valid_attention(int T, int seqs, int max_q, int max_kv, int q_heads, int kv_heads, int d)
+{
+    return T >= 0 && seqs >= 0 && seqs <= 65535 && max_q >= 0 && max_kv >= 0 && max_kv <= (1 << 30) && qvggt::kv4_valid_head(d) && kv_heads >= 1 && kv_heads <= 65535 &&
+           q_heads >= kv_heads && q_heads % kv_heads == 0 && (long long)max_q * (q_heads / kv_heads) <= (1 << 30);
+}
+}  // namespace
+
+size_t qvggt_kv4_page_bytes(int page_tokens, int heads, int d)
+{
+    return valid_pages(0, page_tokens, heads, d) ? (size_t)heads * page_tokens * (d + 4) : 0;
+}
+
+int qvggt_kv4_append(const void *K, const void *V, int x_dtype, int T, long long k_stride, long long v_stride, int heads, int d, const float *rope, int rope_rows, int rope_dim,
+                     int rope_pair, const int32_t *positions, const int8_t *signs, const int32_t *slots, void *cache, int num_pages, int page_tokens, void *stream)
+{
+    if (!valid_dtype(x_dtype)) return QVGGT_ERR_DTYPE;
+    if (!valid_pages(num_pages, page_tokens, heads, d) || !valid_rows(T, heads) || !valid_rope(rope, rope_rows, rope_dim, rope_pair, d) || k_stride < 0 || v_stride < 0)
+        return QVGGT_ERR_SHAPE;
+    if (T == 0 || num_pages == 0) return QVGGT_OK;
+    if (!K || !V || !slots || !cache || (rope && !positions)) return QVGGT_ERR_NULL;
+    const int vector = x_dtype == QVGGT_F32 ? 4 : 8;          // elements of 16 bytes
+    if (!aligned16(K) || !aligned16(V) || k_stride % vector != 0 || v_stride % vector != 0 || !aligned16(rope) || !aligned16(positions) || !aligned16(signs) ||
+        !aligned16(slots) || !aligned16(cache))
+        return QVGGT_ERR_ALIGN;
+    return hip_status(qvggt::run_kv4_append(K, V, x_dtype == QVGGT_F32, T, k_stride, v_stride, d, {rope, positions, rope_rows, rope_dim, rope_pair}, signs, slots,
+                                            pages_of(cache, num_pages, page_tokens, heads), static_cast<hipStream_t>(stream)));
+}
+
+int qvggt_kv4_read(const void *cache, int num_pages, int page_tokens, int heads, int d, const int8_t *signs, const int32_t *slots, int T, int out_dtype, void *K, void *V,
+                   void *stream)
+{
+    if (!valid_dtype(out_dtype)) return QVGGT_ERR_DTYPE;
+    if (!valid_pages(num_pages, page_tokens, heads, d) || !valid_rows(T, heads)) return QVGGT_ERR_SHAPE;
+    if (T == 0 || (!K && !V)) return QVGGT_OK;
+    if (!slots || (num_pages > 0 && !cache)) return QVGGT_ERR_NULL;
+    if (!aligned16(cache) || !aligned16(signs) || !aligned16(slots) || !aligned16(K) || !aligned16(V)) return QVGGT_ERR_ALIGN;
+    return hip_status(qvggt::run_kv4_read(pages_of(cache, num_pages, page_tokens, heads), d, slots, T, signs, out_dtype == QVGGT_F32, K, V, static_cast<hipStream_t>(stream)));
+}
+
+size_t qvggt_kv4_attention_workspace_bytes(int T, int seqs, int max_q, int max_kv, int q_heads, int kv_heads, int d)
+{
+    return valid_attention(T, seqs, max_q, max_kv, q_heads, kv_heads, d) ? qvggt::kv4_attention_workspace_bytes(T, seqs, max_q, max_kv, q_heads, kv_heads, d) : 0;
+}
+
+int qvggt_kv4_attention(const void *Q, int q_dtype, int T, long long q_stride, int q_heads, const float *rope, int rope_rows, int rope_dim, int rope_pair,
+                        const int32_t *positions, const int8_t *signs, float scale, int causal, const void *cache, int num_pages, int page_tokens, int kv_heads, int d,
+                        const int32_t *page_table, int table_width, const int32_t *q_starts, const int32_t *kv_lens, int seqs, int max_q, int max_kv, void *out, void *workspace,
+                        size_t workspace_bytes, void *stream)
+{
+    if (!valid_dtype(q_dtype)) return QVGGT_ERR_DTYPE;
+    if (!valid_pages(num_pages, page_tokens, kv_heads, d) || !valid_attention(T, seqs, max_q, max_kv, q_heads, kv_heads, d) || q_stride < 0 ||
+        !valid_rope(rope, rope_rows, rope_dim, rope_pair, d) || table_width < 0 || max_kv > (long long)table_width * page_tokens || (max_kv > 0 && num_pages == 0))
+        return QVGGT_ERR_SHAPE;
+    if (!std::isfinite(scale) || (causal != 0 && causal != 1)) return QVGGT_ERR_ARG;
+    if (T == 0 || seqs == 0 || max_q == 0) return QVGGT_OK;
+    const size_t need = qvggt::kv4_attention_workspace_bytes(T, seqs, max_q, max_kv, q_heads, kv_heads, d);
+    if (!Q || !q_starts || !kv_lens || !out || (rope && !positions) || (max_kv > 0 && (!cache || !page_table)) || (need > 0 && !workspace)) return QVGGT_ERR_NULL;
+    if (!aligned16(Q) || q_stride % (q_dtype == QVGGT_F32 ? 4 : 8) != 0 || !aligned16(rope) || !aligned16(positions) || !aligned16(signs) || !aligned16(cache) ||
+        !aligned16(page_table) || !aligned16(q_starts) || !aligned16(kv_lens) || !aligned16(out) || !aligned16(workspace))
+        return QVGGT_ERR_ALIGN;
+    if (workspace_bytes < need) return QVGGT_ERR_WORKSPACE;
+    const qvggt::Kv4Attention a{Q, q_dtype == QVGGT_F32, T, q_heads, q_stride, {rope, positions, rope_rows, rope_dim, rope_pair}, signs, scale, causal,
+                                pages_of(cache, num_pages, page_tokens, kv_heads), page_table, table_width, q_starts, kv_lens, seqs, max_q, max_kv,
+                                static_cast<uint16_t *>(out), static_cast<float *>(workspace)};
+    return hip_status(qvggt::run_kv4_attention(a, d, static_cast<hipStream_t>(stream)));
 }
 
 // ---- calibration-set arithmetic (Sec. 3.3)

@@ -1,0 +1,173 @@
+// A paged key/value cache held in 4 bits: where its bytes lie, and what the kernels that write and read it share.
+//
+// A page holds P tokens (a power of two from 16 to 1024) of every head; a head's part of a page is P * (D + 4) bytes, one after another:
+//   the keys' codes     token after token, D / 2 bytes each: channel 2 j in the low half of byte j, 2 j + 1 in the high half
+//   the values' codes   blocks of 16 tokens, 8 D bytes each: [4 groups of 4 tokens][16][D / 32][4 tokens] bytes; a byte is a pair of neighbouring channels of one
+//                       token, pair p at [p / (D / 32)][p % (D / 32)]
+//   the steps           4 bytes a token: the key's step as a bf16 in the low half, the value's in the high half
+// Codes are kept as code + 8.  Both orders are those in which the lanes of a 16 x 16 x 32 matrix instruction want them, so that attention loads a block of 16 tokens as
+// consecutive D / 8 bytes per lane and multiplies what it has loaded: in keys the lane of token t has a quarter of the channels, in values the lane of 16 channels
+// (8 of them in D / 32 words) has a group of 4 tokens.  No byte has two tokens in it: a token is appended without reading its neighbours.
+#pragma once
+#include <type_traits>
+
+#include "qvggt_common.h"
+
+namespace qvggt {
+
+constexpr int kKv4Block = 16;       // tokens of a block
+inline bool kv4_valid_page(int page_tokens) { return page_tokens >= 16 && page_tokens <= 1024 && (page_tokens & (page_tokens - 1)) == 0; }
+inline bool kv4_valid_head(int d) { return d == 64 || d == 128; }
+
+struct Kv4Pages {
+    uint8_t *base;
+    int num_pages, page_shift, heads;      // P = 1 << page_shift
+};
+template <int D>
+struct Kv4Layout {
+    static constexpr int kRow = D / 2;              // bytes of a key
+    static constexpr int kBlock = 8 * D;            // bytes of a block of 16 values
+    static constexpr int kWords = D / 32;           // words of a lane's part of a block
+    // byte offset of a head's part of a page
+    __host__ __device__ static size_t part(int page, int head, int heads, int page_shift) { return ((size_t)page * heads + head) * ((size_t)(D + 4) << page_shift); }
+    __host__ __device__ static int keys(int t) { return t * kRow; }
+    __host__ __device__ static int values(int t, int page_shift) { return (kRow << page_shift) + (t >> 4) * kBlock; }
+    __host__ __device__ static int steps(int t, int page_shift) { return (D << page_shift) + 4 * t; }
+    // byte of channels 2 p and 2 p + 1 of token t (0 .. 15) inside a block of values
+    __host__ __device__ static int value_byte(int t, int p) { return (((t >> 2) * 16 + p / kWords) * kWords + p % kWords) * 4 + (t & 3); }
+};
+
+// The rotation by position: pairs (c, c ^ pair) of the first `dim` channels, angle number (c / (2 pair)) * pair + c % pair of the row positions[token] of the
+// table: [rows][cosines dim / 2, sines dim / 2].  table == nullptr: none.
+struct Rope {
+    const float *table;
+    const int32_t *positions;
+    int rows, dim, pair;
+};
+
+// ---- a row of D channels in 16 lanes, C = D / 16 consecutive channels in each
+template <int C>
+__device__ inline void load_channels(const void *row, bool f32, int first, float (&x)[C])
+{
+    if (f32) {
+        const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(row) + first);
+#pragma unroll
+        for (int i = 0; i < C / 4; ++i) {
+            const float4 v = p[i];
+            x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
+        }
+    } else {
+        const uint2 *p = reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(row) + first);
+        uint32_t w[C / 2];
+        if constexpr (C == 8) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(p);
+            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+        } else {
+            const uint2 v = *p;
+            w[0] = v.x; w[1] = v.y;
+        }
+#pragma unroll
+        for (int i = 0; i < C / 2; ++i) {
+            x[2 * i] = bf16_bits_to_float(w[i] & 0xffffu);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+}
+
+// x[first .. first + C) of `row` rotated for table row `at`.  The partners of channels that other lanes have are loaded a second time.
+template <int C>
+__device__ inline void rotate_channels(const void *row, bool f32, int first, const Rope &rope, int at, float (&x)[C])
+{
+    if (first >= rope.dim) return;                  // dim is a multiple of 16: a lane's channels turn or do not
+    const float *cosines = rope.table + (size_t)at * rope.dim, *sines = cosines + rope.dim / 2;
+    float other[C], c[C], s[C];
+    if (rope.pair >= C) {
+        load_channels<C>(row, f32, first ^ rope.pair, other);
+        const int angle = (first / (2 * rope.pair)) * rope.pair + (first & (rope.pair - 1));
+        load_channels<C>(cosines, true, angle, c);
+        load_channels<C>(sines, true, angle, s);
+        const float sign = (first & rope.pair) ? 1.0f : -1.0f;
+#pragma unroll
+        for (int i = 0; i < C; ++i) x[i] = fmaf(x[i], c[i], sign * s[i] * other[i]);
+    } else {
+        auto within = [&](auto pair) {
+            constexpr int kPair = decltype(pair)::value;
+            float y[C];
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+                const int angle = ((first + i) / (2 * kPair)) * kPair + (i & (kPair - 1));
+                const float sine = sines[angle];
+                y[i] = fmaf(x[i], cosines[angle], ((i & kPair) ? sine : -sine) * x[i ^ kPair]);
+            }
+#pragma unroll
+            for (int i = 0; i < C; ++i) x[i] = y[i];
+        };
+        if (rope.pair == 1) within(std::integral_constant<int, 1>());
+        else if (rope.pair == 2) within(std::integral_constant<int, 2>());
+        else if constexpr (C > 4) within(std::integral_constant<int, 4>());
+    }
+}
+
+template <int C>
+__device__ inline void sign_channels(const int8_t *signs, int first, float (&x)[C])
+{
+    if (signs == nullptr) return;
+#pragma unroll
+    for (int i = 0; i < C / 4; ++i) {
+        const uint32_t w = *reinterpret_cast<const uint32_t *>(signs + first + 4 * i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[4 * i + j] = __uint_as_float(__float_as_uint(x[4 * i + j]) ^ ((w << (24 - 8 * j)) & 0x80000000u));
+    }
+}
+
+// The unnormalised Walsh-Hadamard butterflies of a row, the channel bits in rising order: those inside a lane, then the lane's four (DPP, as in lane_butterflies).
+template <int C>
+__device__ inline void row_butterflies(float (&x)[C], int lane)
+{
+#pragma unroll
+    for (int b = 1; b < C; b *= 2)
+#pragma unroll
+        for (int i = 0; i < C; ++i)
+            if (!(i & b)) {
+                const float u = x[i], v = x[i | b];
+                x[i] = u + v;
+                x[i | b] = u - v;
+            }
+    const float s1 = (lane & 1) ? -1.0f : 1.0f, s2 = (lane & 2) ? -1.0f : 1.0f, s4 = (lane & 4) ? -1.0f : 1.0f, s8 = (lane & 8) ? -1.0f : 1.0f;
+#pragma unroll
+    for (int r = 0; r < C; ++r) {
+        x[r] = fmaf(x[r], s1, dpp_move<0xB1>(x[r]));
+        x[r] = fmaf(x[r], s2, dpp_move<0x4E>(x[r]));
+        x[r] = fmaf(x[r], s4, dpp_move<0x141>(dpp_move<0x1B>(x[r])));
+        x[r] = fmaf(x[r], s8, dpp_move<0x128>(x[r]));
+    }
+}
+
+template <int D>
+constexpr float kv4_norm() { return D == 64 ? 0.125f : 0.08838834764831845f; }       // 1 / sqrt(D)
+
+// host side: the launchers behind the entry points
+hipError_t run_kv4_append(const void *K, const void *V, bool f32, int T, long long k_stride, long long v_stride, int d, const Rope &rope, const int8_t *signs,
+                          const int32_t *slots, const Kv4Pages &pages, hipStream_t stream);
+hipError_t run_kv4_read(const Kv4Pages &pages, int d, const int32_t *slots, int T, const int8_t *signs, bool f32, void *K, void *V, hipStream_t stream);
+
+struct Kv4Attention {
+    const void *q;
+    int q_f32, T, q_heads;
+    long long q_stride;
+    Rope rope;
+    const int8_t *signs;
+    float scale;
+    int causal;
+    Kv4Pages pages;
+    const int32_t *table;
+    int table_width;
+    const int32_t *starts, *lens;
+    int seqs, max_q, max_kv;
+    uint16_t *out;
+    float *partials;
+};
+size_t kv4_attention_workspace_bytes(int T, int seqs, int max_q, int max_kv, int q_heads, int kv_heads, int d);
+hipError_t run_kv4_attention(const Kv4Attention &a, int d, hipStream_t stream);
+
+}  // namespace qvggt
