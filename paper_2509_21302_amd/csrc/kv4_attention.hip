@@ -78,23 +78,91 @@ __device__ inline size_t partial_row(const Kv4Attention &a, int group, int split
     return (((size_t)b * a.pages.heads + head) * ((size_t)a.max_q * group) + row) * splits + split;
 }
 
+// What a wave holds of 32 tokens: words of keys and values and the steps, as they lie in the pages.
+template <int D>
+struct Step {
+    uint32_t k[2][D / 32], v[2][D / 32];
+    uint32_t s[2][4];
+};
+
+// waves that a SIMD's registers hold: as many as leave none of them in scratch memory
+template <int D, int NT>
+constexpr int kWavesPerSimd = NT == 4 ? 1 : NT == 2 ? 2 : D == 64 ? 4 : 3;
+
 // Waves of a block share rows and take steps of 32 keys in turn (SHARE, up to 16 NT rows: few rows, many keys), or have 16 NT rows each.
 template <int D, int NT, bool SHARE>
-__global__ __launch_bounds__(256) void kv4_attention_kernel(Work work)
+__global__ __launch_bounds__(256, (kWavesPerSimd<D, NT>)) void kv4_attention_kernel(Work work)
 {
     using L = Kv4Layout<D>;
     constexpr int C = D / 16, W = L::kWords, S = D / 32;
     constexpr int kPad = D + 4;                             // floats of a row in LDS
+    constexpr int kStride = SHARE ? 128 : 32;               // keys from a wave's step to its next
     __shared__ __align__(16) float area[4][16 * kPad];
     __shared__ float row_max[4][16], row_sum[4][16];
     const Kv4Attention &a = work.a;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n16 = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
     const int split = blockIdx.x % work.splits, tile = blockIdx.x / work.splits;
     const int head = blockIdx.y, b = blockIdx.z, group = work.group;
     const Sequence seq = sequence_of(a, b);
     const int rows = seq.n * group, row0 = SHARE ? tile * 16 * NT : (tile * 4 + wave) * 16 * NT;
     if (SHARE ? row0 >= rows : tile * 64 * NT >= rows) return;
     float *const mine = area[wave];
+
+    // ---- keys of this block
+    const int rows_here = min(max(rows - row0, 0), 16 * NT);
+    const int last = rows_here > 0 ? visible(a, seq, (row0 + rows_here - 1) / group) : 0;       // keys that some row of the wave's sees
+    const int full = rows_here > 0 ? visible(a, seq, row0 / group) : 0;                         // keys that all of them see
+    const int begin = split * work.chunk, stop = min(last, begin + work.chunk);
+    if (SHARE && begin >= last && split > 0) return;            // nobody reads what this split would have left (rows without keys at all: the first split's)
+
+    // The way of a step: its blocks' pages two steps ahead (scalar loads), its bytes into the registers of the step before as soon as those are taken apart.  Blocks behind the end
+    // are taken as the last one.
+    const int page_shift = a.pages.page_shift, page_mask = (1 << page_shift) - 1, last_block = max(last - 1, 0) / 16;
+    const auto *const table = reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(reinterpret_cast<uintptr_t>(a.table + (size_t)b * a.table_width));
+    const size_t part_bytes = (size_t)(D + 4) << page_shift;
+    const uint8_t *const head_base = a.pages.base + head * part_bytes;
+    auto find = [&](int t0, int (&page)[2]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) page[h] = table[min(t0 / 16 + h, last_block) * 16 >> page_shift];
+    };
+    const uint8_t *part[2];                     // the next step's blocks: head parts of pages, and tokens in them
+    int at[2];
+    auto locate = [&](int t0, const int (&page)[2]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            at[h] = min(t0 / 16 + h, last_block) * 16 & page_mask;
+            part[h] = head_base + (size_t)min(max(page[h], 0), a.pages.num_pages - 1) * (a.pages.heads * part_bytes);
+        }
+    };
+    auto words = [&](const uint8_t *from, uint32_t (&w)[W]) {
+        if constexpr (W == 4) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(from);
+            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+        } else {
+            const uint2 v = *reinterpret_cast<const uint2 *>(from);
+            w[0] = v.x; w[1] = v.y;
+        }
+    };
+    const int key_of_lane = n16 * L::kRow + g * 4 * W, value_of_lane = lane * 4 * W;
+    Step<D> x;
+    auto fetch_keys = [&](int h) { words(part[h] + L::keys(at[h]) + key_of_lane, x.k[h]); };
+    auto fetch_values = [&](int h) { words(part[h] + L::values(at[h], page_shift) + value_of_lane, x.v[h]); };
+    auto fetch_steps = [&](int h) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(part[h] + L::steps(at[h], page_shift) + 16 * g);
+        x.s[h][0] = v.x; x.s[h][1] = v.y; x.s[h][2] = v.z; x.s[h][3] = v.w;
+    };
+    int t0 = begin + (SHARE ? wave * 32 : 0), page[2] = {0, 0};
+    if (t0 < stop) {
+        find(t0, page);
+        locate(t0, page);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            fetch_keys(h);
+            fetch_steps(h);
+            fetch_values(h);
+        }
+        find(t0 + kStride, page);
+    }
 
     // ---- queries: four rows at a time to LDS, turned; then the lane's operands.  Lane (n, g) has channels g D / 4 .. of row n, as the keys' lanes have
     Operand q[NT][S];
@@ -105,9 +173,10 @@ __global__ __launch_bounds__(256) void kv4_attention_kernel(Work work)
     for (int j = 0; j < NT; ++j) {
         const int r = row0 + 16 * j + n16;
         end[j] = r < rows ? visible(a, seq, r / group) : 0;
+        float *const turned = SHARE ? area[j & 3] : mine;          // shared rows: a quarter of them by every wave
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int row = row0 + 16 * j + 4 * k + g, first = n16 * C;
+        for (int k = 0; k < (SHARE ? 1 : 4); ++k) {
+            const int r16 = SHARE ? 4 * wave + g : 4 * k + g, row = row0 + 16 * j + r16, first = n16 * C;
             float x[C];
 #pragma unroll
             for (int i = 0; i < C; ++i) x[i] = 0.0f;
@@ -121,16 +190,17 @@ __global__ __launch_bounds__(256) void kv4_attention_kernel(Work work)
             row_butterflies<C>(x, lane);
             const float f = kv4_norm<D>() * a.scale * kLog2e;
 #pragma unroll
-            for (int i = 0; i < C; ++i) mine[(4 * k + g) * kPad + first + i] = x[i] * f;
+            for (int i = 0; i < C; ++i) turned[r16 * kPad + first + i] = x[i] * f;
         }
-        lanes_exchange_fence();
+        if constexpr (SHARE) __syncthreads();
+        else lanes_exchange_fence();
         float x[D / 4], top = 0.0f;
 #pragma unroll
         for (int i = 0; i < D / 4; ++i) {
-            x[i] = mine[n16 * kPad + g * (D / 4) + i];
+            x[i] = turned[n16 * kPad + g * (D / 4) + i];
             top = fmaxf(top, fabsf(x[i]));
         }
-        lanes_exchange_fence();
+        if constexpr (!SHARE) lanes_exchange_fence();
         top = max_over_64_lanes(top);
         // 2^(13 - e) with 2^e <= top < 2^(e + 1): the largest query number of the tile in 2^13 .. 2^14, the others to an absolute error that is 2^-25 of a score unit at least.
         // Numbers over 2^17 (scores in the ten thousands at least: one key takes all the weight) become the largest fp16 and leave the other rows alone
@@ -171,15 +241,9 @@ __global__ __launch_bounds__(256) void kv4_attention_kernel(Work work)
         base[j] = -sum * 0x1p-21f;
     }
 
-    // ---- keys of this block
-    const int rows_here = min(max(rows - row0, 0), 16 * NT);
-    const int last = rows_here > 0 ? visible(a, seq, (row0 + rows_here - 1) / group) : 0;       // keys that some row of the wave's sees
-    const int begin = split * work.chunk, stop = min(last, begin + work.chunk);
-    if (SHARE && begin >= last && split > 0) return;            // nobody reads what this split would have left (rows without keys at all: the first split's)
-
     float4v acc[NT][2 * W], ones[NT];
     float m[NT], l[NT];
-    float reach = 0.0f;                                         // power of two that no value's step so far is above
+    float reach = 0.0f, per = 0.0f;                             // power of two that no value's step so far is above; kTop / reach
     const float4v zero = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
@@ -193,60 +257,55 @@ __global__ __launch_bounds__(256) void kv4_attention_kernel(Work work)
 #pragma unroll
     for (int i = 0; i < 4; ++i) eights.w[i] = 0x00080008u;
 
-    const int page_mask = (1 << a.pages.page_shift) - 1, last_block = (last - 1) / 16;
-    for (int t0 = begin + (SHARE ? wave * 32 : 0); t0 < stop; t0 += SHARE ? 128 : 32) {
-        uint32_t kw[2][W], vw[2][W];
+    // 32 keys; edge: some row does not see all of them
+    auto take = [&](auto edge) {
+        constexpr bool kEdge = decltype(edge)::value;
         float ks[2][4], vs[2][4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int block = min(t0 / 16 + h, last_block), t = 16 * block;
-            const int entry = a.table[(size_t)b * a.table_width + (t >> a.pages.page_shift)];
-            const int page = min(max(entry, 0), a.pages.num_pages - 1);
-            const uint8_t *const part = a.pages.base + L::part(page, head, a.pages.heads, a.pages.page_shift);
-            const uint8_t *kp = part + L::keys((t & page_mask) + n16) + g * 4 * W, *vp = part + L::values(t & page_mask, a.pages.page_shift) + lane * 4 * W;
-            const uint4 st = *reinterpret_cast<const uint4 *>(part + L::steps((t & page_mask) + 4 * g, a.pages.page_shift));
-            if constexpr (W == 4) {
-                const uint4 k = *reinterpret_cast<const uint4 *>(kp), v = *reinterpret_cast<const uint4 *>(vp);
-                kw[h][0] = k.x; kw[h][1] = k.y; kw[h][2] = k.z; kw[h][3] = k.w;
-                vw[h][0] = v.x; vw[h][1] = v.y; vw[h][2] = v.z; vw[h][3] = v.w;
-            } else {
-                const uint2 k = *reinterpret_cast<const uint2 *>(kp), v = *reinterpret_cast<const uint2 *>(vp);
-                kw[h][0] = k.x; kw[h][1] = k.y;
-                vw[h][0] = v.x; vw[h][1] = v.y;
-            }
-            const uint32_t sw[4] = {st.x, st.y, st.z, st.w};
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const bool there = t0 + 16 * h + 4 * g + i < last;             // behind the end lies whatever was there: no number, perhaps
-                ks[h][i] = bf16_bits_to_float(sw[i] & 0xffffu) * unit;
-                vs[h][i] = there ? __uint_as_float(sw[i] & 0xffff0000u) : 0.0f;
+                ks[h][i] = __uint_as_float(x.s[h][i] << 16) * unit;
+                vs[h][i] = __uint_as_float(x.s[h][i] & 0xffff0000u);
+                if (kEdge && t0 + 16 * h + 4 * g + i >= last) vs[h][i] = 0.0f;             // behind the end lies whatever was there: no number, perhaps
             }
-        }
-        // scores, in powers of two
-        float t[NT][2][4], tops = 0.0f, over = kNone;
+        locate(t0 + kStride, page);
+        find(t0 + 2 * kStride, page);
+        // scores, in powers of two above the running maximum
+        float4v sc[NT][2];
+        float t[NT][2][4], over = kNone, tops = 0.0f;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             Operand k[S];
 #pragma unroll
             for (int s = 0; s < S; ++s) {
-                const uint32_t w = kw[h][s], u = w >> 8;
+                const uint32_t w = x.k[h][s], u = w >> 8;
                 k[s].w[0] = w & kLow; k[s].w[1] = w & kHigh; k[s].w[2] = u & kLow; k[s].w[3] = u & kHigh;
             }
+            fetch_keys(h);
+            fetch_steps(h);
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                float4v x = {base[j], base[j], base[j], base[j]};
+                sc[j][h] = float4v{base[j], base[j], base[j], base[j]};
 #pragma unroll
-                for (int s = 0; s < S; ++s) x = mfma(k[s], q[j][s], x);
+                for (int s = 0; s < S; ++s) sc[j][h] = mfma(k[s], q[j][s], sc[j][h]);
+            }
+        }
+        auto above = [&](int j, int h, int i) {
+            const float v = fmaf(sc[j][h][i], ks[h][i], -m[j]);
+            return kEdge && t0 + 16 * h + 4 * g + i >= end[j] ? -INFINITY : v;
+        };
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const bool seen = t0 + 16 * h + 4 * g + i < end[j];
-                    t[j][h][i] = seen ? x[i] * ks[h][i] : -INFINITY;
-                    over = fmaxf(over, t[j][h][i] - m[j]);
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                tops = fmaxf(tops, vs[h][i]);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    t[j][h][i] = above(j, h, i);
+                    over = fmaxf(over, t[j][h][i]);
                 }
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) tops = fmaxf(tops, vs[h][i]);
-        }
         if (__builtin_amdgcn_ballot_w64(over > kSlack || tops > reach)) {
             tops = max_over_64_lanes(tops);
             float shrink = 1.0f;
@@ -254,17 +313,18 @@ __global__ __launch_bounds__(256) void kv4_attention_kernel(Work work)
                 const float up = __uint_as_float(min((__float_as_uint(tops) & 0x7f800000u) + 0x00800000u, 0x7f000000u));
                 shrink = reach / up;
                 reach = up;
+                per = kTop / up;
             }
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                float top = kNone;
+                float top = m[j];
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) top = fmaxf(top, t[j][h][i]);
+                    for (int i = 0; i < 4; ++i)
+                        if (!kEdge || t0 + 16 * h + 4 * g + i < end[j]) top = fmaxf(top, sc[j][h][i] * ks[h][i]);
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
-                top = fmaxf(top, m[j]);
                 const float down = __builtin_amdgcn_exp2f(m[j] - top);
                 m[j] = top;
                 l[j] *= down;
@@ -275,11 +335,14 @@ __global__ __launch_bounds__(256) void kv4_attention_kernel(Work work)
                 for (int c = 0; c < 2 * W; ++c)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) acc[j][c][i] *= both;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) t[j][h][i] = above(j, h, i);
             }
         }
         // weights: tokens 0, 2 and 1, 3 of a group of four, as the bytes of a value's word come apart
         Operand p[NT];
-        const float per = reach > 0.0f ? kTop / reach : 0.0f;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             float f[4];
@@ -289,13 +352,10 @@ __global__ __launch_bounds__(256) void kv4_attention_kernel(Work work)
             for (int j = 0; j < NT; ++j) {
                 float e[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    e[i] = __builtin_amdgcn_exp2f(t[j][h][i] - m[j]);
-                    l[j] += e[i];
-                    e[i] *= f[i];
-                }
-                p[j].w[2 * h] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(e[0], e[2]));
-                p[j].w[2 * h + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(e[1], e[3]));
+                for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(t[j][h][i]);
+                l[j] += (e[0] + e[1]) + (e[2] + e[3]);
+                p[j].w[2 * h] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(e[0] * f[0], e[2] * f[2]));
+                p[j].w[2 * h + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(e[1] * f[1], e[3] * f[3]));
             }
         }
 #pragma unroll
@@ -303,9 +363,9 @@ __global__ __launch_bounds__(256) void kv4_attention_kernel(Work work)
             Operand low, high;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const uint32_t x = vw[h][w], u = x >> 8;
-                low.w[2 * h] = x & kLow; low.w[2 * h + 1] = u & kLow;
-                high.w[2 * h] = x & kHigh; high.w[2 * h + 1] = u & kHigh;
+                const uint32_t v = x.v[h][w], u = v >> 8;
+                low.w[2 * h] = v & kLow; low.w[2 * h + 1] = u & kLow;
+                high.w[2 * h] = v & kHigh; high.w[2 * h + 1] = u & kHigh;
             }
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
@@ -313,12 +373,17 @@ __global__ __launch_bounds__(256) void kv4_attention_kernel(Work work)
                 acc[j][2 * w + 1] = mfma(high, p[j], acc[j][2 * w + 1]);
             }
         }
+        fetch_values(0);
+        fetch_values(1);
 #pragma unroll
         for (int j = 0; j < NT; ++j) ones[j] = mfma(eights, p[j], ones[j]);
-    }
+    };
+    for (const int whole = min(full, stop) - 32; t0 <= whole; t0 += kStride) take(std::false_type());       // (one loop with both in it takes 70 registers more)
+    for (; t0 < stop; t0 += kStride) take(std::true_type());
 
     // ---- sums to LDS, row by row: lane (n, g) has channels 2 W (4 g + i) + c of row n
     const float back = reach * (0x1p24f / kTop);
+    if constexpr (SHARE) __syncthreads();                       // the area had the queries
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
         l[j] += __shfl_xor(l[j], 16);
@@ -373,27 +438,57 @@ __global__ __launch_bounds__(256) void kv4_attention_kernel(Work work)
     }
 }
 
-// The splits of a row put together: 16 lanes have a row.
+// The splits of a row put together: a block has a row, 16 lanes of it every sixteenth split.
 template <int D>
 __global__ __launch_bounds__(256) void kv4_join_kernel(Work work)
 {
     constexpr int C = D / 16;
+    __shared__ __align__(16) float sums[16][D + 4];
+    __shared__ float tops[16], totals[16];
     const Kv4Attention &a = work.a;
-    const int lane = threadIdx.x & 63, first = (lane & 15) * C, head = blockIdx.y, b = blockIdx.z, row = blockIdx.x * 16 + (threadIdx.x >> 4);
+    const int lane = threadIdx.x & 63, first = (lane & 15) * C, part = threadIdx.x >> 4, head = blockIdx.y, b = blockIdx.z, row = blockIdx.x;
     const Sequence seq = sequence_of(a, b);
     if (row >= seq.n * work.group) return;
     const int end = visible(a, seq, row / work.group), used = (end + work.chunk - 1) / work.chunk;
     const float *const from = a.partials + partial_row(a, work.group, work.splits, b, head, row, 0) * kPartial<D>;
     float top = kNone, total = 0.0f, x[C];
-    for (int s = 0; s < used; ++s) top = fmaxf(top, from[(size_t)s * kPartial<D> + D]);
 #pragma unroll
     for (int i = 0; i < C; ++i) x[i] = 0.0f;
-    for (int s = 0; s < used; ++s) {
+    for (int s = part; s < used; s += 16) {
         const float *p = from + (size_t)s * kPartial<D>;
-        const float f = __builtin_amdgcn_exp2f(p[D] - top);
-        total = fmaf(f, p[D + 1], total);
+        const float2 end_of = *reinterpret_cast<const float2 *>(p + D);
+        float y[C];
 #pragma unroll
-        for (int i = 0; i < C; ++i) x[i] = fmaf(f, p[first + i], x[i]);
+        for (int i = 0; i < C / 2; ++i) {
+            const float2 v = reinterpret_cast<const float2 *>(p + first)[i];
+            y[2 * i] = v.x;
+            y[2 * i + 1] = v.y;
+        }
+        const float above = fmaxf(top, end_of.x), f = __builtin_amdgcn_exp2f(end_of.x - above), down = __builtin_amdgcn_exp2f(top - above);
+        top = above;
+        total = fmaf(f, end_of.y, total * down);
+#pragma unroll
+        for (int i = 0; i < C; ++i) x[i] = fmaf(f, y[i], x[i] * down);
+    }
+#pragma unroll
+    for (int i = 0; i < C; ++i) sums[part][first + i] = x[i];
+    if ((lane & 15) == 0) {
+        tops[part] = top;
+        totals[part] = total;
+    }
+    __syncthreads();
+    if (part != 0) return;
+    top = tops[0];
+#pragma unroll
+    for (int p = 1; p < 16; ++p) top = fmaxf(top, tops[p]);
+    total = 0.0f;
+#pragma unroll
+    for (int i = 0; i < C; ++i) x[i] = 0.0f;
+    for (int p = 0; p < min(used, 16); ++p) {
+        const float f = __builtin_amdgcn_exp2f(tops[p] - top);
+        total = fmaf(f, totals[p], total);
+#pragma unroll
+        for (int i = 0; i < C; ++i) x[i] = fmaf(f, sums[p][first + i], x[i]);
     }
     finish_row<D>(a, work.group, seq, head, row, x, total > 0.0f || total != total ? kv4_norm<D>() / total : 0.0f, lane);
 }
@@ -413,7 +508,8 @@ Plan plan_of(int seqs, int max_q, int max_kv, int q_heads, int kv_heads)
     const int per_block = p.share ? 16 * p.nt : 64 * p.nt;
     p.tiles_of_rows = (int)((rows + per_block - 1) / per_block);
     const long long blocks = (long long)p.tiles_of_rows * kv_heads * seqs;
-    long long splits = 1024 / (blocks > 0 ? blocks : 1);
+    // blocks that share rows: 512 fill the chip's registers once (131071 keys of one sequence: 32 us, 36 with 1024 blocks, 45 with 2048); the others are fewer than that only for few rows
+    long long splits = (p.share ? 512 : 1024) / (blocks > 0 ? blocks : 1);
     const int least = p.share ? 128 : 512;
     const long long most = (max_kv + least - 1) / least;
     if (splits > most) splits = most;
@@ -437,7 +533,7 @@ hipError_t launch(const Kv4Attention &a, hipStream_t stream)
     else kv4_attention_kernel<D, 2, false><<<grid, 256, 0, stream>>>(w);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
-    kv4_join_kernel<D><<<dim3((a.max_q * w.group + 15) / 16, a.pages.heads, a.seqs), 256, 0, stream>>>(w);
+    kv4_join_kernel<D><<<dim3(a.max_q * w.group, a.pages.heads, a.seqs), 256, 0, stream>>>(w);
     return hipGetLastError();
 }
 
