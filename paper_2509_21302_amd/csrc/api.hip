@@ -902,7 +902,7 @@ int qvggt_kv4_read(const void *cache, int num_pages, int page_tokens, int heads,
 
 size_t qvggt_kv4_attention_workspace_bytes(int T, int seqs, int max_q, int max_kv, int q_heads, int kv_heads, int d)
 {
-    return valid_attention(T, seqs, max_q, max_kv, q_heads, kv_heads, d) ? qvggt::kv4_attention_workspace_bytes(T, seqs, max_q, max_kv, q_heads, kv_heads, d) : 0;
+    return valid_attention(T, seqs, max_q, max_kv, q_heads, kv_heads, d) ? qvggt::kv4_attention_workspace_bytes(seqs, max_q, max_kv, q_heads, kv_heads, d) : 0;
 }
 
 int qvggt_kv4_attention(const void *Q, int q_dtype, int T, long long q_stride, int q_heads, const float *rope, int rope_rows, int rope_dim, int rope_pair,
@@ -916,7 +916,7 @@ int qvggt_kv4_attention(const void *Q, int q_dtype, int T, long long q_stride, i
         return QVGGT_ERR_SHAPE;
     if (!std::isfinite(scale) || (causal != 0 && causal != 1)) return QVGGT_ERR_ARG;
     if (T == 0 || seqs == 0 || max_q == 0) return QVGGT_OK;
-    const size_t need = qvggt::kv4_attention_workspace_bytes(T, seqs, max_q, max_kv, q_heads, kv_heads, d);
+    const size_t need = qvggt::kv4_attention_workspace_bytes(seqs, max_q, max_kv, q_heads, kv_heads, d);
     if (!Q || !q_starts || !kv_lens || !out || (rope && !positions) || (max_kv > 0 && (!cache || !page_table)) || (need > 0 && !workspace)) return QVGGT_ERR_NULL;
     if (!aligned16(Q) || q_stride % (q_dtype == QVGGT_F32 ? 4 : 8) != 0 || !aligned16(rope) || !aligned16(positions) || !aligned16(signs) || !aligned16(cache) ||
         !aligned16(page_table) || !aligned16(q_starts) || !aligned16(kv_lens) || !aligned16(out) || !aligned16(workspace))
@@ -924,7 +924,7 @@ int qvggt_kv4_attention(const void *Q, int q_dtype, int T, long long q_stride, i
     if (workspace_bytes < need) return QVGGT_ERR_WORKSPACE;
     const qvggt::Kv4Attention a{Q, q_dtype == QVGGT_F32, T, q_heads, q_stride, {rope, positions, rope_rows, rope_dim, rope_pair}, signs, scale, causal,
                                 pages_of(cache, num_pages, page_tokens, kv_heads), page_table, table_width, q_starts, kv_lens, seqs, max_q, max_kv,
-                                static_cast<uint16_t *>(out), static_cast<float *>(workspace)};
+                                static_cast<uint16_t *>(out), workspace};
     return hip_status(qvggt::run_kv4_attention(a, d, static_cast<hipStream_t>(stream)));
 }
 

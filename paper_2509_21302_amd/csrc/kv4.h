@@ -45,68 +45,113 @@ struct Rope {
     int rows, dim, pair;
 };
 
-// ---- a row of D channels in 16 lanes, C = D / 16 consecutive channels in each
+// ---- a row of D channels in 16 lanes, C = D / 16 consecutive channels in each, as it comes from memory: loads that depend on nothing first, those that need the
+// position next, arithmetic last, so that a wave waits for memory twice and not once for every operand
 template <int C>
-__device__ inline void load_channels(const void *row, bool f32, int first, float (&x)[C])
-{
-    if (f32) {
-        const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(row) + first);
+struct HeadRow {
+    // channels, and the ones they turn with where other lanes have those (bf16: half of the words).  All of it starts from something: what one path only sets would be kept in registers
+    // from one turn of a surrounding loop to the next
+    uint32_t x[C] = {}, partner[C] = {};
+    float cosine[C] = {}, sine[C] = {};
+    uint32_t sign[C / 4] = {};
+    int at = 0;
+
+    __device__ static void words(const void *row, bool f32, int first, uint32_t (&w)[C])
+    {
+        if (f32) {
 #pragma unroll
-        for (int i = 0; i < C / 4; ++i) {
-            const float4 v = p[i];
-            x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
-        }
-    } else {
-        const uint2 *p = reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(row) + first);
-        uint32_t w[C / 2];
-        if constexpr (C == 8) {
-            const uint4 v = *reinterpret_cast<const uint4 *>(p);
+            for (int i = 0; i < C / 4; ++i) {
+                const uint4 v = reinterpret_cast<const uint4 *>(static_cast<const float *>(row) + first)[i];
+                w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+            }
+        } else if constexpr (C == 8) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(row) + first);
             w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
         } else {
-            const uint2 v = *p;
+            const uint2 v = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(row) + first);
             w[0] = v.x; w[1] = v.y;
         }
+    }
+    __device__ static void floats(const uint32_t (&w)[C], bool f32, float (&y)[C])
+    {
 #pragma unroll
-        for (int i = 0; i < C / 2; ++i) {
-            x[2 * i] = bf16_bits_to_float(w[i] & 0xffffu);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        for (int i = 0; i < C; ++i) y[i] = f32 ? __uint_as_float(w[i]) : __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    }
+    __device__ void load(const void *row, bool f32, int first, const int8_t *signs)
+    {
+        words(row, f32, first, x);
+        if (signs != nullptr) {
+#pragma unroll
+            for (int i = 0; i < C / 4; ++i) sign[i] = reinterpret_cast<const uint32_t *>(signs + first)[i];
         }
     }
-}
-
-// x[first .. first + C) of `row` rotated for table row `at`.  The partners of channels that other lanes have are loaded a second time.
-template <int C>
-__device__ inline void rotate_channels(const void *row, bool f32, int first, const Rope &rope, int at, float (&x)[C])
-{
-    if (first >= rope.dim) return;                  // dim is a multiple of 16: a lane's channels turn or do not
-    const float *cosines = rope.table + (size_t)at * rope.dim, *sines = cosines + rope.dim / 2;
-    float other[C], c[C], s[C];
-    if (rope.pair >= C) {
-        load_channels<C>(row, f32, first ^ rope.pair, other);
-        const int angle = (first / (2 * rope.pair)) * rope.pair + (first & (rope.pair - 1));
-        load_channels<C>(cosines, true, angle, c);
-        load_channels<C>(sines, true, angle, s);
-        const float sign = (first & rope.pair) ? 1.0f : -1.0f;
+    __device__ void load_turn(const void *row, bool f32, int first, const Rope &rope, long long token)
+    {
+        if (rope.table == nullptr) return;
+        at = rope.positions[token];
+        if (rope.pair >= C) words(row, f32, first ^ rope.pair, partner);
+    }
+    __device__ void load_angles(int first, const Rope &rope)
+    {
+        if (rope.table == nullptr) return;
+        // dim is a multiple of 16: a lane's channels turn or do not (those take the first ones' angles, for nothing).  C consecutive angles, or half as many where pairs are inside a lane
+        const int c = first < rope.dim ? first : 0;
+        const bool wide = rope.pair >= C;
+        const int angle = wide ? (c / (2 * rope.pair)) * rope.pair + (c & (rope.pair - 1)) : c / 2;
+        const float *from = rope.table + (size_t)min(max(at, 0), rope.rows - 1) * rope.dim + angle;
 #pragma unroll
-        for (int i = 0; i < C; ++i) x[i] = fmaf(x[i], c[i], sign * s[i] * other[i]);
-    } else {
-        auto within = [&](auto pair) {
-            constexpr int kPair = decltype(pair)::value;
-            float y[C];
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int i = 0; i < C; ++i) {
-                const int angle = ((first + i) / (2 * kPair)) * kPair + (i & (kPair - 1));
-                const float sine = sines[angle];
-                y[i] = fmaf(x[i], cosines[angle], ((i & kPair) ? sine : -sine) * x[i ^ kPair]);
+            for (int i = 0; i < C / 4; ++i) {
+                const int k = (wide && h ? C / 2 : 0) + 2 * i, to = h * (C / 2) + 2 * i;
+                const float2 u = *reinterpret_cast<const float2 *>(from + k), v = *reinterpret_cast<const float2 *>(from + rope.dim / 2 + k);
+                cosine[to] = u.x; cosine[to + 1] = u.y;
+                sine[to] = v.x; sine[to + 1] = v.y;
+            }
+    }
+    __device__ void channels(bool f32, int first, const int8_t *signs, float (&y)[C]) const
+    {
+        floats(x, f32, y);
+        if (signs != nullptr) flip(y);
+    }
+    // ... turned
+    __device__ void turned(bool f32, int first, const Rope &rope, const int8_t *signs, float (&y)[C]) const
+    {
+        floats(x, f32, y);
+        if (rope.table != nullptr) {
+            const bool inside = first < rope.dim;
+            float z[C];
+            if (rope.pair >= C) {
+                const float side = (first & rope.pair) ? 1.0f : -1.0f;
+                float other[C];
+                floats(partner, f32, other);
+#pragma unroll
+                for (int i = 0; i < C; ++i) z[i] = fmaf(y[i], cosine[i], side * sine[i] * other[i]);
+            } else {
+                auto within = [&](auto pair) {
+                    constexpr int kPair = decltype(pair)::value;
+#pragma unroll
+                    for (int i = 0; i < C; ++i) {
+                        constexpr int kAll = 2 * kPair;
+                        const int angle = i / kAll * kPair + i % kPair;
+                        z[i] = fmaf(y[i], cosine[angle], ((i & kPair) ? sine[angle] : -sine[angle]) * y[i ^ kPair]);
+                    }
+                };
+                if (rope.pair == 1) within(std::integral_constant<int, 1>());
+                else if (rope.pair == 2) within(std::integral_constant<int, 2>());
+                else within(std::integral_constant<int, C / 2>());
             }
 #pragma unroll
-            for (int i = 0; i < C; ++i) x[i] = y[i];
-        };
-        if (rope.pair == 1) within(std::integral_constant<int, 1>());
-        else if (rope.pair == 2) within(std::integral_constant<int, 2>());
-        else if constexpr (C > 4) within(std::integral_constant<int, 4>());
+            for (int i = 0; i < C; ++i) y[i] = inside ? z[i] : y[i];
+        }
+        if (signs != nullptr) flip(y);
     }
-}
+    __device__ void flip(float (&y)[C]) const
+    {
+#pragma unroll
+        for (int i = 0; i < C; ++i) y[i] = __uint_as_float(__float_as_uint(y[i]) ^ ((sign[i / 4] << (24 - 8 * (i % 4))) & 0x80000000u));
+    }
+};
 
 template <int C>
 __device__ inline void sign_channels(const int8_t *signs, int first, float (&x)[C])
@@ -165,9 +210,9 @@ struct Kv4Attention {
     const int32_t *starts, *lens;
     int seqs, max_q, max_kv;
     uint16_t *out;
-    float *partials;
+    void *workspace;
 };
-size_t kv4_attention_workspace_bytes(int T, int seqs, int max_q, int max_kv, int q_heads, int kv_heads, int d);
+size_t kv4_attention_workspace_bytes(int seqs, int max_q, int max_kv, int q_heads, int kv_heads, int d);
 hipError_t run_kv4_attention(const Kv4Attention &a, int d, hipStream_t stream);
 
 }  // namespace qvggt

@@ -54,14 +54,18 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(const void *K, const vo
     if (slot < 0 || slot >= (long long)pages.num_pages << pages.page_shift) return;
     const int elem = f32 ? 4 : 2, t = slot & ((1 << pages.page_shift) - 1);
     uint8_t *const part = pages.base + L::part(slot >> pages.page_shift, head, pages.heads, pages.page_shift);
+    const char *k_row = static_cast<const char *>(K) + (token * k_stride + (long long)head * D) * elem, *v_row = static_cast<const char *>(V) + (token * v_stride + (long long)head * D) * elem;
+    HeadRow<C> key, value;
+    key.load(k_row, f32, first, signs);
+    key.load_turn(k_row, f32, first, rope, token);
+    value.load(v_row, f32, first, signs);
+    key.load_angles(first, rope);
     uint32_t steps = 0;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-        const char *row = static_cast<const char *>(which ? V : K) + (token * (which ? v_stride : k_stride) + (long long)head * D) * elem;
         float x[C];
-        load_channels<C>(row, f32, first, x);
-        if (which == 0 && rope.table != nullptr) rotate_channels<C>(row, f32, first, rope, min(max(rope.positions[token], 0), rope.rows - 1), x);
-        sign_channels<C>(signs, first, x);
+        if (which == 0) key.turned(f32, first, rope, signs, x);
+        else value.channels(f32, first, signs, x);
         row_butterflies<C>(x, lane);
 #pragma unroll
         for (int i = 0; i < C; ++i) x[i] *= kv4_norm<D>();

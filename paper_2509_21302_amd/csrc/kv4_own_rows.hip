@@ -1,0 +1,132 @@
+// Attention over the 4-bit key/value cache for more rows than the waves of a block share (prompts, queries on another sequence's states): a wave has 32 rows of its own and goes through all
+// keys that they see; the four waves of a block go through the same pages at about the same time.
+#include "kv4_attention.h"
+#include "kv4_plan.h"
+
+namespace qvggt {
+namespace {
+
+struct Tiled {
+    Kv4Attention a;
+    int group, chunk, splits;           // query heads of a key head; keys of a part, and how many parts there may be
+    float *partials;                    // [seqs][heads][rows][splits][D + 2]
+};
+__device__ inline size_t partial_row(const Tiled &w, int b, int head, int row, int split)
+{
+    return (((size_t)b * w.a.pages.heads + head) * ((size_t)w.a.max_q * w.group) + row) * w.splits + split;
+}
+
+constexpr int kTiles = 2;               // of 16 rows a wave
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void kv4_own_rows_kernel(Tiled w)
+{
+    constexpr int C = D / 16, kPad = D + 4, NT = kTiles;
+    __shared__ __align__(16) float area[4][16 * kPad];
+    __shared__ float tops[4][16], totals[4][16];
+    const Kv4Attention &a = w.a;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
+    const int split = blockIdx.x % w.splits, tile = blockIdx.x / w.splits, head = blockIdx.y, b = blockIdx.z;
+    const Sequence seq = sequence_of(a, b);
+    const int rows = seq.n * w.group, row0 = (tile * 4 + wave) * 16 * NT, here = min(rows - row0, 16 * NT);
+    if (here <= 0) return;
+    const int last = visible(a, seq, (row0 + here - 1) / w.group), full = visible(a, seq, row0 / w.group);      // keys that some row sees, and that all see
+    const int t0 = split * w.chunk, stop = min(last, t0 + w.chunk);
+    typedef Rows<D, NT, 1, false> Mine;
+    Mine r;
+    float *const mine = area[wave];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        typename Mine::Query query[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) query[k].load(a, seq, head, w.group, row0 + 16 * j + 4 * k + g, rows, lane);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) query[k].load_angles(a, lane);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) query[k].store(a, row0 + 16 * j + 4 * k + g < rows, mine + (4 * k + g) * kPad, lane);
+        lanes_exchange_fence();
+        const int row = row0 + 16 * j + (lane & 15);
+        r.end[j] = row < rows ? visible(a, seq, row / w.group) : 0;
+        r.take_queries(j, mine, lane);
+        lanes_exchange_fence();
+    }
+    r.start();
+    Keys<D, 1, false> keys;
+    if (t0 < stop) keys.begin(a, b, head, last, t0, 32, lane);
+    r.run(keys, t0, 32, full, last, stop, g);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        r.leave(j, mine, tops[wave], totals[wave], lane);
+        lanes_exchange_fence();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int r16 = 4 * k + g, row = row0 + 16 * j + r16, first = (lane & 15) * C;
+            float x[C];
+#pragma unroll
+            for (int i = 0; i < C; ++i) x[i] = mine[r16 * kPad + first + i];
+            if (row < rows) {
+                if (w.splits == 1) finish_row<D>(a, w.group, seq, head, row, x, totals[wave][r16], lane);
+                else leave_row<D>(w.partials + partial_row(w, b, head, row, split) * kPartial<D>, x, tops[wave][r16], totals[wave][r16], lane);
+            }
+        }
+        lanes_exchange_fence();
+    }
+}
+
+// The parts of a row put together: 16 lanes have a row.
+template <int D>
+__global__ __launch_bounds__(256) void kv4_join_parts_kernel(Tiled w)
+{
+    constexpr int C = D / 16;
+    const Kv4Attention &a = w.a;
+    const int lane = threadIdx.x & 63, first = (lane & 15) * C, head = blockIdx.y, b = blockIdx.z, row = blockIdx.x * 16 + (threadIdx.x >> 4);
+    const Sequence seq = sequence_of(a, b);
+    if (row >= seq.n * w.group) return;
+    const int used = (visible(a, seq, row / w.group) + w.chunk - 1) / w.chunk;
+    const float *const from = w.partials + partial_row(w, b, head, row, 0) * kPartial<D>;
+    float top = kNone, total = 0.0f, x[C];
+    for (int s = 0; s < used; ++s) top = fmaxf(top, from[(size_t)s * kPartial<D> + D]);
+#pragma unroll
+    for (int i = 0; i < C; ++i) x[i] = 0.0f;
+    for (int s = 0; s < used; ++s) {
+        const float *p = from + (size_t)s * kPartial<D>;
+        const float f = __builtin_amdgcn_exp2f(p[D] - top);
+        total = fmaf(f, p[D + 1], total);
+#pragma unroll
+        for (int i = 0; i < C; ++i) x[i] = fmaf(f, p[first + i], x[i]);
+    }
+    finish_row<D>(a, w.group, seq, head, row, x, total, lane);
+}
+
+template <int D>
+hipError_t launch(const Kv4Attention &a, hipStream_t stream)
+{
+    const int group = a.q_heads / a.pages.heads;
+    const Kv4Tiles p = kv4_tiles(a.seqs, a.max_q, a.max_kv, a.q_heads, a.pages.heads, D, 64 * kTiles);
+    const Tiled w{a, group, p.chunk, p.splits, static_cast<float *>(a.workspace)};
+    kv4_own_rows_kernel<D><<<dim3(p.tiles * p.splits, a.pages.heads, a.seqs), 256, 0, stream>>>(w);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.splits == 1) return e;
+    kv4_join_parts_kernel<D><<<dim3((a.max_q * group + 15) / 16, a.pages.heads, a.seqs), 256, 0, stream>>>(w);
+    return hipGetLastError();
+}
+
+hipError_t run_kv4_own_rows(const Kv4Attention &a, int d, hipStream_t stream) { return d == 64 ? launch<64>(a, stream) : launch<128>(a, stream); }
+
+}  // namespace
+
+hipError_t run_kv4_shared_rows(const Kv4Attention &a, int d, hipStream_t stream);
+
+size_t kv4_attention_workspace_bytes(int seqs, int max_q, int max_kv, int q_heads, int kv_heads, int d)
+{
+    if ((long long)max_q * (q_heads / kv_heads) <= kKv4SharedRows) return kv4_shares(seqs, max_q, max_kv, q_heads, kv_heads, d).bytes;
+    return kv4_tiles(seqs, max_q, max_kv, q_heads, kv_heads, d, 64 * kTiles).bytes;
+}
+
+hipError_t run_kv4_attention(const Kv4Attention &a, int d, hipStream_t stream)
+{
+    if ((long long)a.max_q * (a.q_heads / a.pages.heads) <= kKv4SharedRows) return run_kv4_shared_rows(a, d, stream);
+    return run_kv4_own_rows(a, d, stream);
+}
+
+}  // namespace qvggt
