@@ -54,6 +54,10 @@ LINEAR_KINDS = ("qvggt_linear", "qvggt_linear_e2m3_any", "qvggt_gelu_linear_e2m3
 PACKED, E2M3, GELU, INT8, INT8_BLOCKS = range(5)
 
 
+# ... and those that its functions of their own call, in its order
+KV4 = ("qvggt_kv4_append", "qvggt_kv4_read", "qvggt_kv4_attention")
+
+
 class QvggtError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -212,6 +216,8 @@ def load_library() -> C.CDLL:
     if _call is not None:
         for kind, name in enumerate(LINEAR_KINDS):
             _call.bind(kind, C.cast(getattr(lib, name), C.c_void_p).value)
+        for which, name in enumerate(KV4):
+            _call.bind_kv4(which, C.cast(getattr(lib, name), C.c_void_p).value)
     _lib = lib
     return lib
 
@@ -685,11 +691,25 @@ def _pool_of(cache, page_tokens, heads, d):
     return _ptr(cache), cache.numel() // size
 
 
+def _native(function, name, *args) -> bool:
+    """Whether _call has taken a call.  What it does not know, the function below it takes, or refuses."""
+    if _lib is None:
+        load_library()
+    status = function(*args)
+    if status is NotImplemented:
+        return False
+    if status:
+        raise QvggtError(status, name)
+    return True
+
+
 def qvggt_kv4_page_bytes(page_tokens: int, heads: int, d: int) -> int:
     return int(load_library().qvggt_kv4_page_bytes(int(page_tokens), int(heads), int(d)))
 
 
 def qvggt_kv4_append(K, V, signs, slots, cache, page_tokens, rope=None, positions=None, rope_pair=0, stream=None):
+    if stream is None and _call is not None and _native(_call.kv4_append, "qvggt_kv4_append", K, V, signs, slots, cache, page_tokens, rope, positions, rope_pair):
+        return
     T, heads, d = K.shape
     if V.shape != K.shape or V.dtype != K.dtype:
         raise ValueError("V: the shape and type of K")
@@ -703,6 +723,8 @@ def qvggt_kv4_append(K, V, signs, slots, cache, page_tokens, rope=None, position
 
 
 def qvggt_kv4_read(cache, page_tokens, signs, slots, K, V, stream=None):
+    if stream is None and _call is not None and _native(_call.kv4_read, "qvggt_kv4_read", cache, page_tokens, signs, slots, K, V):
+        return
     out = K if K is not None else V
     T, heads, d = out.shape
     if K is not None and V is not None and (V.shape != K.shape or V.dtype != K.dtype):
@@ -718,6 +740,9 @@ def qvggt_kv4_attention_workspace_bytes(T: int, seqs: int, max_q: int, max_kv: i
 
 def qvggt_kv4_attention(Q, signs, scale, causal, cache, page_tokens, kv_heads, page_table, q_starts, kv_lens, max_q, max_kv, out, workspace, rope=None,
                         positions=None, rope_pair=0, stream=None):
+    if stream is None and _call is not None and _native(_call.kv4_attention, "qvggt_kv4_attention", Q, signs, scale, causal, cache, page_tokens, kv_heads, page_table, q_starts, kv_lens,
+                                                        max_q, max_kv, out, workspace, rope, positions, rope_pair):
+        return
     T, heads, d = Q.shape
     at_q, q_stride = _heads_of(Q, "Q")
     if out.shape != Q.shape or out.dtype != torch.bfloat16:
