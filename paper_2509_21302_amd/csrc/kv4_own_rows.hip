@@ -8,7 +8,7 @@ namespace {
 
 struct Tiled {
     Kv4Attention a;
-    int group, chunk, splits;           // query heads of a key head; keys of a part, and how many parts there may be
+    int group, chunk, splits, tiles;    // query heads of a key head; keys of a part; parts and tiles of rows that there may be
     float *partials;                    // [seqs][heads][rows][splits][D + 2]
 };
 __device__ inline size_t partial_row(const Tiled &w, int b, int head, int row, int split)
@@ -26,10 +26,13 @@ __global__ __launch_bounds__(256, 2) void kv4_own_rows_kernel(Tiled w)
     __shared__ float tops[4][16], totals[4][16];
     const Kv4Attention &a = w.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
-    const int split = blockIdx.x % w.splits, tile = blockIdx.x / w.splits, head = blockIdx.y, b = blockIdx.z;
+    // Heads first, parts next, then tiles from the last one on, where rows see most, sequences last: blocks that run together have keys in common (those of a head on one of the eight
+    // dies, where heads are a multiple of eight), and a sequence's longest blocks begin first
+    const int head = blockIdx.x % a.pages.heads, rest = blockIdx.x / a.pages.heads, b = rest / (w.tiles * w.splits), place = rest % (w.tiles * w.splits);
     const Sequence seq = sequence_of(a, b);
-    const int rows = seq.n * w.group, row0 = (tile * 4 + wave) * 16 * NT, here = min(rows - row0, 16 * NT);
-    if (here <= 0) return;
+    const int rows = seq.n * w.group, tile = (rows + 64 * NT - 1) / (64 * NT) - 1 - place / w.splits, split = place % w.splits;
+    const int row0 = (tile * 4 + wave) * 16 * NT, here = min(rows - row0, 16 * NT);
+    if (tile < 0 || here <= 0) return;
     const int last = visible(a, seq, (row0 + here - 1) / w.group), full = visible(a, seq, row0 / w.group);      // keys that some row sees, and that all see
     const int t0 = split * w.chunk, stop = min(last, t0 + w.chunk);
     typedef Rows<D, NT, 1, false> Mine;
@@ -103,8 +106,8 @@ hipError_t launch(const Kv4Attention &a, hipStream_t stream)
 {
     const int group = a.q_heads / a.pages.heads;
     const Kv4Tiles p = kv4_tiles(a.seqs, a.max_q, a.max_kv, a.q_heads, a.pages.heads, D, 64 * kTiles);
-    const Tiled w{a, group, p.chunk, p.splits, static_cast<float *>(a.workspace)};
-    kv4_own_rows_kernel<D><<<dim3(p.tiles * p.splits, a.pages.heads, a.seqs), 256, 0, stream>>>(w);
+    const Tiled w{a, group, p.chunk, p.splits, p.tiles, static_cast<float *>(a.workspace)};
+    kv4_own_rows_kernel<D><<<dim3((unsigned)a.seqs * a.pages.heads * p.tiles * p.splits), 256, 0, stream>>>(w);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
     kv4_join_parts_kernel<D><<<dim3((a.max_q * group + 15) / 16, a.pages.heads, a.seqs), 256, 0, stream>>>(w);
