@@ -32,7 +32,8 @@ constexpr uint32_t kLow = 0x000f000fu, kHigh = 0x00f000f0u;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNone = -1e30f;                 // running maximum of a row that has seen nothing
 constexpr float kSlack = 8.0f;                  // weights may pass 1 by this many powers of two before sums are scaled down
-constexpr float kTop = 128.0f;                  // weight of a score at the running maximum with the largest step: 2^15 with the slack, under fp16's 65504
+constexpr int kTop = 7;                         // log2 of a weight at the running maximum with the largest step: 2^15 with the slack, under fp16's 65504
+constexpr int kSmallest = -90;                  // log2 of the least largest step that weights are scaled up for (fp32 sums of 2^20 of them stay in range)
 
 // what a block knows about its sequence
 struct Sequence {
@@ -161,10 +162,14 @@ struct Rows {
     Operand q[NT][S];
     float base[NT];                     // what the first product starts from: -8 times the sum of the queries
     int end[NT];                        // keys that the lane's row sees
-    float exponent[NT], unit;           // of a product of a query number and a subnormal
+    int exponent[NT], unit;             // log2 of a tile's unit; of the product of a query number and a subnormal, 0 .. 27, in a float's exponent
+    // Weights are 2^(score - m): m is the running maximum less `lift`, by which weights times steps fill fp16's range (kTop below the top at a step of `reach`, a power of two that no
+    // value's step so far is above).  l: their sum; acc, ones: their sums times step times code + 8, and times step times 8.  Whatever the lift, sums over l are the result.
     float4v acc[NT][2 * W], ones[NT];
     float m[NT], l[NT];
-    float reach, per;                   // power of two that no value's step so far is above; kTop / reach
+    float reach, lift;
+    uint32_t seen;                      // bit j: the lane's row of tile j has a maximum (or will never have one)
+    float unseen;                       // infinite until all have
 
     // A row of queries on its way to LDS: what 16 lanes load of it (rows behind the last one: the last one), and the row turned.
     struct Query {
@@ -200,8 +205,8 @@ struct Rows {
         top = max_over_64_lanes(top);
         // 2^(13 - e) with 2^e <= top < 2^(e + 1): the largest query number of the tile in 2^13 .. 2^14, the others to an absolute error that is 2^-25 of a score unit at least.
         // Numbers over 2^17 (scores in the ten thousands at least: one key takes all the weight) become the largest fp16 and leave the other rows alone
-        const int e = min(max((int)(__float_as_uint(top) >> 23), 20), 127 + 16);
-        exponent[j] = (float)(e - 127 - 13);
+        const int e = min(max((int)(__float_as_uint(top) >> 23), 127 - 11), 127 + 16);
+        exponent[j] = e - 127 - 13;
         const float up = __uint_as_float((uint32_t)(127 + 13 - (e - 127)) << 23);
 #pragma unroll
         for (int s = 0; s < S; ++s) {
@@ -217,17 +222,21 @@ struct Rows {
             for (int i = 0; i < 8; ++i) q[j][s].h[i] = (_Float16)y[order[i]];
         }
     }
-    // all tiles on one power of two, and nothing seen yet
-    __device__ void start()
+    __device__ int highest_exponent() const
     {
-        float highest = exponent[0];
+        int highest = exponent[0];
 #pragma unroll
-        for (int j = 1; j < NT; ++j) highest = fmaxf(highest, exponent[j]);
-        unit = __builtin_amdgcn_exp2f(highest + 24.0f);
+        for (int j = 1; j < NT; ++j) highest = max(highest, exponent[j]);
+        return highest;
+    }
+    // all tiles on one power of two, and nothing seen yet
+    __device__ void start(int highest)
+    {
+        unit = (highest + 24) << 23;
         const float4v zero = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            const _Float16 down = (_Float16)__builtin_amdgcn_exp2f(fmaxf(exponent[j] - highest, -40.0f));
+            const _Float16 down = (_Float16)__builtin_amdgcn_exp2f((float)(exponent[j] - highest));
             float sum = 0.0f;
 #pragma unroll
             for (int s = 0; s < S; ++s)
@@ -242,12 +251,65 @@ struct Rows {
 #pragma unroll
             for (int c = 0; c < 2 * W; ++c) acc[j][c] = zero;
             ones[j] = zero;
-            m[j] = kNone;
-            l[j] = 0.0f;
+            m[j] = l[j] = 0.0f;
         }
-        reach = per = 0.0f;
+        reach = lift = 0.0f;
+        seen = 0;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) seen |= (uint32_t)(end[j] == 0) << j;
+        unseen = INFINITY;
     }
-
+    // t: the scores of a step above m, -inf where a row does not see a key.  Where one is above the maximum by more than the slack, a value's step above all before, or a row without
+    // a maximum: maxima and lift anew, and t and the sums with them.  (Scores are got back from t: nothing else of the step is kept for this.)
+    __device__ void raise(float (&t)[NT][2][4], float over, float tops)
+    {
+        if (!__builtin_amdgcn_ballot_w64(over > kSlack + lift || tops > reach)) return;
+        tops = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(max_over_64_lanes(tops))));        // (reach and lift stay scalar)
+        const float before = lift;
+        if (tops > reach) {
+            const int e = max((int)(__float_as_uint(tops) >> 23) - 126, kSmallest);            // 2^e > tops
+            reach = __uint_as_float((uint32_t)(min(e, 127) + 127) << 23);
+            lift = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int((float)(kTop - e))));
+        }
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, t[j][h][i]);
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const bool first = !(seen >> j & 1), any = top > -INFINITY;
+            const float up = first ? (any ? top - lift : 0.0f) : fmaxf(top, before) - lift;                 // (t has the lift in it)
+            const float down = first ? 1.0f : __builtin_amdgcn_exp2f(-up);                    // (a first maximum: there are no sums yet)
+            seen |= (uint32_t)any << j;
+            m[j] += up;
+            l[j] *= down;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) t[j][h][i] -= up;
+            ones[j] *= down;
+#pragma unroll
+            for (int c = 0; c < 2 * W; ++c) acc[j][c] *= down;
+        }
+        unseen = seen == (1u << NT) - 1 ? kNone : INFINITY;
+    }
+    // A tile's weights of 32 keys from their scores above m: their sum, and with the values' steps the operand of the second product.  Tokens 0, 2 and 1, 3 of a group of four lie
+    // together, as the bytes of a value's word come apart.
+    __device__ void weigh(int j, const float (&t)[2][4], const float (&vs)[2][4], Operand &p)
+    {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float e[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(t[h][i]);
+            l[j] += (e[0] + e[1]) + (e[2] + e[3]);
+            p.w[2 * h] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(e[0] * vs[h][0], e[2] * vs[h][2]));
+            p.w[2 * h + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(e[1] * vs[h][1], e[3] * vs[h][3]));
+        }
+    }
     // The 32 keys from t0, which `x` holds in place d, and the fetch of those AHEAD steps on.  EDGE: some row does not see all of them; last: keys that some row sees.
     template <bool EDGE>
     __device__ void take(Keys<D, AHEAD, ONCE> &x, int d, int t0, int stride, int last, int g)
@@ -257,7 +319,7 @@ struct Rows {
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                ks[h][i] = __uint_as_float(x.s[d][h][i] << 16) * unit;
+                ks[h][i] = __uint_as_float((x.s[d][h][i] << 16) + unit);          // times a power of two (a step 0: some 2^-100)
                 vs[h][i] = __uint_as_float(x.s[d][h][i] & 0xffff0000u);
                 if (EDGE && t0 + 16 * h + 4 * g + i >= last) vs[h][i] = 0.0f;             // behind the end lies whatever was there: no number, perhaps
             }
@@ -265,28 +327,32 @@ struct Rows {
         x.find(t0 + (AHEAD + 1) * stride);
         // scores, in powers of two above the running maximum
         float4v sc[NT][2];
-        float t[NT][2][4], over = kNone, tops = 0.0f;
+        float t[NT][2][4], over = unseen, tops = 0.0f;
+        auto product = [&](int h, int s) {
+            Operand k;
+            const uint32_t w = x.k[d][h][s], u = w >> 8;
+            k.w[0] = w & kLow; k.w[1] = w & kHigh; k.w[2] = u & kLow; k.w[3] = u & kHigh;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            Operand k[S];
+            for (int j = 0; j < NT; ++j) sc[j][h] = mfma(k, q[j][s], s == 0 ? float4v{base[j], base[j], base[j], base[j]} : sc[j][h]);
+        };
+        // One tile: the two blocks in turn, a product need not wait for the one before (64 sequences to 8192 keys 76 -> 69 us); several tiles are turns enough, and block after
+        // block lets go of registers earlier (prompt of 12289 tokens 1.29 ms, 1.32 the other way)
+        if constexpr (NT == 1) {
 #pragma unroll
             for (int s = 0; s < S; ++s) {
-                const uint32_t w = x.k[d][h][s], u = w >> 8;
-                k[s].w[0] = w & kLow; k[s].w[1] = w & kHigh; k[s].w[2] = u & kLow; k[s].w[3] = u & kHigh;
+                product(0, s);
+                product(1, s);
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if constexpr (NT > 1) {
+#pragma unroll
+                for (int s = 0; s < S; ++s) product(h, s);
             }
             x.fetch_keys(d, h);
             x.fetch_steps(d, h);
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                sc[j][h] = float4v{base[j], base[j], base[j], base[j]};
-#pragma unroll
-                for (int s = 0; s < S; ++s) sc[j][h] = mfma(k[s], q[j][s], sc[j][h]);
-            }
         }
-        auto above = [&](int j, int h, int i) {
-            const float y = fmaf(sc[j][h][i], ks[h][i], -m[j]);
-            return EDGE && t0 + 16 * h + 4 * g + i >= end[j] ? -INFINITY : y;
-        };
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -294,62 +360,15 @@ struct Rows {
                 tops = fmaxf(tops, vs[h][i]);
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
-                    t[j][h][i] = above(j, h, i);
+                    t[j][h][i] = fmaf(sc[j][h][i], ks[h][i], -m[j]);
+                    if (EDGE && t0 + 16 * h + 4 * g + i >= end[j]) t[j][h][i] = -INFINITY;
                     over = fmaxf(over, t[j][h][i]);
                 }
             }
-        if (__builtin_amdgcn_ballot_w64(over > kSlack || tops > reach)) {
-            tops = max_over_64_lanes(tops);
-            float shrink = 1.0f;
-            if (tops > reach) {
-                const float up = __uint_as_float(min((__float_as_uint(tops) & 0x7f800000u) + 0x00800000u, 0x7f000000u));
-                shrink = reach / up;
-                reach = up;
-                per = kTop / up;
-            }
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                float top = m[j];
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (!EDGE || t0 + 16 * h + 4 * g + i < end[j]) top = fmaxf(top, sc[j][h][i] * ks[h][i]);
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(top, __shfl_xor(top, 32));
-                const float down = __builtin_amdgcn_exp2f(m[j] - top);
-                m[j] = top;
-                l[j] *= down;
-                const float both = down * shrink;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) ones[j][i] *= both;
-#pragma unroll
-                for (int c = 0; c < 2 * W; ++c)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[j][c][i] *= both;
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) t[j][h][i] = above(j, h, i);
-            }
-        }
-        // weights: tokens 0, 2 and 1, 3 of a group of four, as the bytes of a value's word come apart
+        raise(t, over, tops);
         Operand p[NT];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float f[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) f[i] = vs[h][i] * per;
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                float e[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(t[j][h][i]);
-                l[j] += (e[0] + e[1]) + (e[2] + e[3]);
-                p[j].w[2 * h] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(e[0] * f[0], e[2] * f[2]));
-                p[j].w[2 * h + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(e[1] * f[1], e[3] * f[3]));
-            }
-        }
+        for (int j = 0; j < NT; ++j) weigh(j, t[j], vs, p[j]);
 #pragma unroll
         for (int w = 0; w < W; ++w) {
             Operand low, high;
@@ -391,7 +410,6 @@ struct Rows {
     __device__ void leave(int j, float *rows16, float *tops, float *totals, int lane)
     {
         const int n = lane & 15, g = lane >> 4;
-        const float back = reach * (0x1p24f / kTop);
         float total = l[j];
         total += __shfl_xor(total, 16);
         total += __shfl_xor(total, 32);
@@ -400,11 +418,11 @@ struct Rows {
 #pragma unroll
             for (int w = 0; w < W; ++w) {
                 float *to = rows16 + n * kPad + 2 * W * (4 * g + i) + 2 * w;
-                to[0] = (acc[j][2 * w][i] - ones[j][i]) * back;
-                to[1] = (acc[j][2 * w + 1][i] * 0.0625f - ones[j][i]) * back;
+                to[0] = (acc[j][2 * w][i] - ones[j][i]) * 0x1p24f;
+                to[1] = (acc[j][2 * w + 1][i] * 0.0625f - ones[j][i]) * 0x1p24f;
             }
         if (g == 0) {
-            tops[n] = m[j];
+            tops[n] = seen >> j & 1 ? m[j] : kNone;
             totals[n] = total;
         }
     }

@@ -1,4 +1,4 @@
-// Attention over the 4-bit key/value cache for more rows than the waves of a block share (prompts, queries on another sequence's states): a wave has 32 rows of its own and goes through all
+// Attention over the 4-bit key/value cache for more rows than the waves of a block share (prompts, queries on another sequence's states): a wave has 32 or 64 rows of its own and goes through all
 // keys that they see; the four waves of a block go through the same pages at about the same time.
 #include "kv4_attention.h"
 #include "kv4_plan.h"
@@ -16,12 +16,10 @@ __device__ inline size_t partial_row(const Tiled &w, int b, int head, int row, i
     return (((size_t)b * w.a.pages.heads + head) * ((size_t)w.a.max_q * w.group) + row) * w.splits + split;
 }
 
-constexpr int kTiles = 2;               // of 16 rows a wave
-
-template <int D>
-__global__ __launch_bounds__(256, 2) void kv4_own_rows_kernel(Tiled w)
+template <int D, int NT>
+__global__ __launch_bounds__(256, (D == 64 && NT == 2 ? 3 : 2)) void kv4_own_rows_kernel(Tiled w)
 {
-    constexpr int C = D / 16, kPad = D + 4, NT = kTiles;
+    constexpr int C = D / 16, kPad = D + 4;
     __shared__ __align__(16) float area[4][16 * kPad];
     __shared__ float tops[4][16], totals[4][16];
     const Kv4Attention &a = w.a;
@@ -53,7 +51,7 @@ __global__ __launch_bounds__(256, 2) void kv4_own_rows_kernel(Tiled w)
         r.take_queries(j, mine, lane);
         lanes_exchange_fence();
     }
-    r.start();
+    r.start(r.highest_exponent());
     Keys<D, 1, false> keys;
     if (t0 < stop) keys.begin(a, b, head, last, t0, 32, lane);
     r.run(keys, t0, 32, full, last, stop, g);
@@ -105,9 +103,11 @@ template <int D>
 hipError_t launch(const Kv4Attention &a, hipStream_t stream)
 {
     const int group = a.q_heads / a.pages.heads;
-    const Kv4Tiles p = kv4_tiles(a.seqs, a.max_q, a.max_kv, a.q_heads, a.pages.heads, D, 64 * kTiles);
+    const Kv4Tiles p = kv4_tiles(a.seqs, a.max_q, a.max_kv, a.q_heads, a.pages.heads, D);
     const Tiled w{a, group, p.chunk, p.splits, p.tiles, static_cast<float *>(a.workspace)};
-    kv4_own_rows_kernel<D><<<dim3((unsigned)a.seqs * a.pages.heads * p.tiles * p.splits), 256, 0, stream>>>(w);
+    const dim3 grid((unsigned)a.seqs * a.pages.heads * p.tiles * p.splits);
+    if (D == 64 && p.nt == 4) kv4_own_rows_kernel<64, 4><<<grid, 256, 0, stream>>>(w);
+    else kv4_own_rows_kernel<D, 2><<<grid, 256, 0, stream>>>(w);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
     kv4_join_parts_kernel<D><<<dim3((a.max_q * group + 15) / 16, a.pages.heads, a.seqs), 256, 0, stream>>>(w);
@@ -123,7 +123,7 @@ hipError_t run_kv4_shared_rows(const Kv4Attention &a, int d, hipStream_t stream)
 size_t kv4_attention_workspace_bytes(int seqs, int max_q, int max_kv, int q_heads, int kv_heads, int d)
 {
     if ((long long)max_q * (q_heads / kv_heads) <= kKv4SharedRows) return kv4_shares(seqs, max_q, max_kv, q_heads, kv_heads, d).bytes;
-    return kv4_tiles(seqs, max_q, max_kv, q_heads, kv_heads, d, 64 * kTiles).bytes;
+    return kv4_tiles(seqs, max_q, max_kv, q_heads, kv_heads, d).bytes;
 }
 
 hipError_t run_kv4_attention(const Kv4Attention &a, int d, hipStream_t stream)

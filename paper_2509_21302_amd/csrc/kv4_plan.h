@@ -10,16 +10,18 @@ constexpr int kKv4SharedRows = 64;          // rows of a key head (query tokens 
 
 // ---- shared rows: every block an even share of all keys
 struct Kv4Shares {
+    int nt, tiles;              // tiles of 16 rows a block takes at a time, and how often that is a head's rows
     int blocks;                 // 0: a block for every head of every sequence, nothing to join
     int unit_shift, least;      // log2 of the keys of a unit; units of a share at least
     size_t map_bytes, bytes;    // workspace: the map of units, all of it
 };
 inline Kv4Shares kv4_shares(int seqs, int max_q, int max_kv, int q_heads, int kv_heads, int d)
 {
-    const int rows = max_q * (q_heads / kv_heads), tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    const int resident = 256 * (tiles == 1 ? (d == 64 ? 4 : 3) : tiles == 2 ? 2 : 1);           // blocks that the chip's registers hold at a time
-    const long long segments = (long long)seqs * kv_heads;
-    Kv4Shares p{0, 7, 4, 0, 0};
+    // Two tiles at most: four take the registers of two waves (64 rows on 16384 keys of 16 sequences, 128 channels: 154 us, where 32 rows are 60)
+    const int rows = max_q * (q_heads / kv_heads);
+    Kv4Shares p{rows <= 16 ? 1 : 2, (rows + 31) / 32, 0, 7, 4, 0, 0};
+    const int resident = 256 * (p.nt == 1 ? 3 : 2);           // blocks that the chip's registers hold at a time
+    const long long segments = (long long)seqs * kv_heads * p.tiles;
     while (segments * (kv4_div_up(max_kv, 1LL << p.unit_shift) + 4) >= 1LL << 30) ++p.unit_shift;
     const long long units = segments * kv4_div_up(max_kv, 1LL << p.unit_shift);
     // Whole heads: where even the longest is not worth a join, and where the blocks are many enough to even out by themselves
@@ -27,29 +29,44 @@ inline Kv4Shares kv4_shares(int seqs, int max_q, int max_kv, int q_heads, int kv
     const long long blocks = kv4_div_up(units, p.least);
     p.blocks = (int)(blocks < resident ? blocks : resident);
     p.map_bytes = (size_t)kv4_div_up(4LL * (1 + seqs), 256) * 256;
-    p.bytes = p.map_bytes + (size_t)p.blocks * 2 * rows * (d + 2) * sizeof(float);
+    p.bytes = p.map_bytes + (size_t)p.blocks * 2 * (16 * p.nt) * (d + 2) * sizeof(float);
     return p;
 }
 
 // ---- a wave's own rows: blocks of 64 NT rows, over a part of the keys each where there are few blocks
 struct Kv4Tiles {
+    int nt;                     // tiles of 16 rows a wave has
     int tiles, chunk, splits;   // blocks of rows; keys of a part, and how many of those the longest sequence has
     size_t bytes;
 };
-inline Kv4Tiles kv4_tiles(int seqs, int max_q, int max_kv, int q_heads, int kv_heads, int d, int rows_of_block)
+inline Kv4Tiles kv4_tiles(int seqs, int max_q, int max_kv, int q_heads, int kv_heads, int d)
 {
     Kv4Tiles p;
-    p.tiles = (int)kv4_div_up((long long)max_q * (q_heads / kv_heads), rows_of_block);
-    const long long blocks = (long long)p.tiles * kv_heads * seqs;
-    constexpr int kLeast = 512;
-    long long splits = blocks > 0 ? 1024 / blocks : 1;
-    const long long most = kv4_div_up(max_kv, kLeast);
-    splits = splits > most ? most : splits;
-    splits = splits < 1 ? 1 : splits;
-    p.chunk = (int)(kv4_div_up(kv4_div_up(max_kv, splits), kLeast) * kLeast);
-    p.chunk = p.chunk < kLeast ? kLeast : p.chunk;
-    p.splits = (int)kv4_div_up(max_kv, p.chunk);
-    p.splits = p.splits < 1 ? 1 : p.splits;
+    const long long rows = (long long)max_q * (q_heads / kv_heads), pairs = (long long)seqs * kv_heads;
+    // 64 channels: four tiles take a key apart half as often as two (a frame over 50: 638 us for 697), but two have half the blocks' length to even out (448 queries on 1500 keys
+    // of 12 sequences: 58 us for 83).  128 channels: the registers hold two
+    const bool fits = 8 * kv4_div_up(rows, 256) * 256 <= 9 * kv4_div_up(rows, 128) * 128;       // few rows more than there are
+    p.nt = d == 64 && fits && (max_kv >= 8192 || kv4_div_up(rows, 256) * pairs >= 2048) ? 4 : 2;
+    p.tiles = (int)kv4_div_up(rows, 64 * p.nt);
+    const int resident = 256 * (p.nt == 2 && d == 64 ? 3 : 2);          // blocks that the chip's registers hold at a time
+    const double blocks = (double)p.tiles * pairs;
+    // How many parts: turns of the resident blocks times a part's keys and what a block costs besides, and the partial sums to memory and back; in units of a key's 40 ns
+    constexpr int kLeast = 128, kMostSplits = 32;
+    double best = 0.0;
+    p.splits = 0;
+    for (int n = 1; n <= kMostSplits && (n == 1 || kv4_div_up(max_kv, n) >= kLeast); ++n) {
+        const int chunk = (int)(kv4_div_up(kv4_div_up(max_kv, n), kLeast) * kLeast);
+        double turns = blocks * n / resident;
+        turns = turns > 2.0 ? turns + 0.5 : (double)(int)(turns + 0.999);
+        const double join = n == 1 ? 0.0 : 200.0 + (double)pairs * rows * n * (d + 2) * 8 / 4.5e6 / 0.04;
+        const double cost = turns * (chunk + 300) + join;
+        if (p.splits == 0 || cost < best) {
+            best = cost;
+            p.chunk = chunk < kLeast ? kLeast : chunk;
+            p.splits = n;
+        }
+    }
+    p.splits = max_kv > 0 ? (int)kv4_div_up(max_kv, p.chunk) : 1;
     p.bytes = p.splits == 1 ? 0 : (size_t)seqs * q_heads * max_q * p.splits * (d + 2) * sizeof(float);
     return p;
 }

@@ -13,9 +13,10 @@ namespace {
 struct Shared {
     Kv4Attention a;
     int group, unit_shift;      // query heads of a key head; log2 of the keys of a unit
+    int tiles, tile_rows;       // tiles of rows of a key head, and rows of one: what is said of a head below is said of each of its tiles
     int blocks, least;          // shares, and the fewest units of one; blocks = 0: a block for every head
     int32_t *map;               // [0]: units of a share, [1 + b]: what one head of all sequences before b costs
-    float *partials;            // [blocks][a head that began in an earlier block, one that goes on in a later one][rows][D + 2]
+    float *partials;            // [blocks][a head that began in an earlier block, one that goes on in a later one][rows of a tile][D + 2]
 };
 
 // What a head of a sequence costs, in units: its keys (one unit at least where it has queries: a head without keys gets its zeros from a block), and in front of them what
@@ -67,20 +68,17 @@ struct Map {
     }
 };
 
-// Waves of a SIMD for 16 rows.  Steps two and three ahead, with fewer waves for their registers, are no faster (64 sequences to 8192 keys 89, 90 and 93 us with two waves): what is in flight is
-// enough.
-template <int D>
-constexpr int kShareWaves = D == 64 ? 4 : 3;
-
+// Three waves a SIMD for 16 rows, two for 32.  Steps two and three ahead, with fewer waves for their registers, are no faster (64 sequences to 8192 keys, 128 channels, two waves: 89, 90
+// and 93 us); four waves for 64 channels leave some registers in scratch memory (48 sequences to 16384 keys, own heads: 94 us for 91).
 template <int D, int NT>
-__global__ __launch_bounds__(256, (NT == 1 ? kShareWaves<D> : NT == 2 ? 2 : 1)) void kv4_shared_rows_kernel(Shared w)
+__global__ __launch_bounds__(256, (NT == 1 ? 3 : 2)) void kv4_shared_rows_kernel(Shared w)
 {
     constexpr int C = D / 16, kPad = D + 4;
     __shared__ __align__(16) float area[4][16 * kPad];
     __shared__ float tops[4][16], totals[4][16];
     __shared__ Map::Place places[4];
     const Kv4Attention &a = w.a;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), heads = a.pages.heads;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tiles = NT == 1 ? 1 : w.tiles, heads = a.pages.heads * tiles;
     const int thread = threadIdx.x;
     Map map{&places[wave], 0, 0, 0};
     int pos = 0, stop = 1;
@@ -125,11 +123,17 @@ __global__ __launch_bounds__(256, (NT == 1 ? kShareWaves<D> : NT == 2 ? 2 : 1)) 
             seq = sequence_of(a, b);
             if (seq.n == 0) return;
         }
-        const int rows = seq.n * w.group, last = seq.len, full = visible(a, seq, 0);
+        const int tile = head % tiles, row0 = tile * 16 * NT, rows = seq.n * w.group;
+        head /= tiles;
+        if (row0 >= rows) {                     // a sequence of fewer rows
+            pos += part;
+            continue;
+        }
+        const int last = seq.len, full = visible(a, seq, row0 / w.group);
         const int t0 = (unit << w.unit_shift) + wave * 32, end = w.blocks > 0 ? min(last, (unit + part) << w.unit_shift) : last;
         Keys<D, 1, true> keys;
         if (last == 0) {                        // nothing is seen: zeros
-            for (int row = 4 * wave + g; row < rows; row += 16) {
+            for (int row = row0 + 4 * wave + g; row < min(rows, row0 + 16 * NT); row += 16) {
                 float x[C] = {};
                 finish_row<D>(a, w.group, seq, head, row, x, 0.0f, lane);
             }
@@ -139,28 +143,28 @@ __global__ __launch_bounds__(256, (NT == 1 ? kShareWaves<D> : NT == 2 ? 2 : 1)) 
         typedef Rows<D, NT, 1, true> Mine;
         typename Mine::Query query[NT];
 #pragma unroll
-        for (int j = 0; j < NT; ++j) query[j].load(a, seq, head, w.group, 16 * j + 4 * wave + g, rows, lane);
+        for (int j = 0; j < NT; ++j) query[j].load(a, seq, head, w.group, row0 + 16 * j + 4 * wave + g, rows, lane);
 #pragma unroll
         for (int j = 0; j < NT; ++j) query[j].load_angles(a, lane);
         keys.begin(a, b, head, last, t0, 128, lane);                   // (a wave that has no step here fetches the last blocks)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) query[j].store(a, 16 * j + 4 * wave + g < rows, area[j] + (4 * wave + g) * kPad, lane);
+        for (int j = 0; j < NT; ++j) query[j].store(a, row0 + 16 * j + 4 * wave + g < rows, area[j] + (4 * wave + g) * kPad, lane);
         Mine r;
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            const int row = 16 * j + (lane & 15);
+            const int row = row0 + 16 * j + (lane & 15);
             r.end[j] = row < rows ? visible(a, seq, row / w.group) : 0;
             r.take_queries(j, area[j], lane);
         }
-        r.start();
+        r.start(r.highest_exponent());
         r.run(keys, t0, 128, full, last, end, g);
         __syncthreads();                        // the area had the queries
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
             r.leave(j, area[wave], tops[wave], totals[wave], lane);
             __syncthreads();
-            const int r16 = 4 * wave + g, row = 16 * j + r16, first = (lane & 15) * C;
+            const int r16 = 4 * wave + g, row = row0 + 16 * j + r16, first = (lane & 15) * C;
             const float top = fmaxf(fmaxf(tops[0][r16], tops[1][r16]), fmaxf(tops[2][r16], tops[3][r16]));
             float x[C], total = 0.0f;
 #pragma unroll
@@ -174,7 +178,7 @@ __global__ __launch_bounds__(256, (NT == 1 ? kShareWaves<D> : NT == 2 ? 2 : 1)) 
             }
             if (row < rows) {
                 if (part == units) finish_row<D>(a, w.group, seq, head, row, x, total, lane);
-                else leave_row<D>(w.partials + ((size_t)(2 * blockIdx.x + (unit == 0)) * (a.max_q * w.group) + row) * kPartial<D>, x, top, total, lane);
+                else leave_row<D>(w.partials + ((size_t)(2 * blockIdx.x + (unit == 0)) * (16 * NT) + row - row0) * kPartial<D>, x, top, total, lane);
             }
             __syncthreads();
         }
@@ -193,7 +197,7 @@ __global__ __launch_bounds__(256) void kv4_join_shares_kernel(Shared w)
     const int lane = threadIdx.x & 63, first = (lane & 15) * C, part = threadIdx.x >> 4, head = blockIdx.y, b = blockIdx.z, row = blockIdx.x;
     const int share = w.map[0], before = w.map[1 + b];
     const Sequence seq = sequence_of(a, b);
-    const int cost = cost_of(w, seq), end = before * a.pages.heads + (head + 1) * cost;
+    const int cost = cost_of(w, seq), tile = row / w.tile_rows, end = before * a.pages.heads * w.tiles + (head * w.tiles + tile + 1) * cost;
     const int from = (end - cost + kSetup) / share, used = (end - 1) / share - from + 1;
     if (row >= seq.n * w.group || used == 1) return;
     float top = kNone, total = 0.0f, x[C];
@@ -205,7 +209,7 @@ __global__ __launch_bounds__(256) void kv4_join_shares_kernel(Shared w)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const int s = min(s0 + 16 * k, used - 1);
-            const float *p = w.partials + ((size_t)(2 * (from + s) + (s == 0)) * (a.max_q * w.group) + row) * kPartial<D>;
+            const float *p = w.partials + ((size_t)(2 * (from + s) + (s == 0)) * w.tile_rows + row - tile * w.tile_rows) * kPartial<D>;
             tail[k] = *reinterpret_cast<const float2 *>(p + D);
             if (s0 + 16 * k >= used) tail[k] = make_float2(kNone, 0.0f);
 #pragma unroll
@@ -256,11 +260,10 @@ hipError_t launch(const Kv4Attention &a, hipStream_t stream)
 {
     const int group = a.q_heads / a.pages.heads, rows = a.max_q * group;
     const Kv4Shares p = kv4_shares(a.seqs, a.max_q, a.max_kv, a.q_heads, a.pages.heads, D);
-    Shared w{a, group, p.unit_shift, p.blocks, p.least, reinterpret_cast<int32_t *>(a.workspace), reinterpret_cast<float *>(static_cast<char *>(a.workspace) + p.map_bytes)};
-    const dim3 grid(p.blocks > 0 ? p.blocks : a.seqs * a.pages.heads);
-    if (rows <= 16) kv4_shared_rows_kernel<D, 1><<<grid, 256, 0, stream>>>(w);
-    else if (rows <= 32) kv4_shared_rows_kernel<D, 2><<<grid, 256, 0, stream>>>(w);
-    else kv4_shared_rows_kernel<D, 4><<<grid, 256, 0, stream>>>(w);
+    Shared w{a, group, p.unit_shift, p.tiles, 16 * p.nt, p.blocks, p.least, reinterpret_cast<int32_t *>(a.workspace), reinterpret_cast<float *>(static_cast<char *>(a.workspace) + p.map_bytes)};
+    const dim3 grid(p.blocks > 0 ? p.blocks : a.seqs * a.pages.heads * p.tiles);
+    if (p.nt == 1) kv4_shared_rows_kernel<D, 1><<<grid, 256, 0, stream>>>(w);
+    else kv4_shared_rows_kernel<D, 2><<<grid, 256, 0, stream>>>(w);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.blocks == 0) return e;
     kv4_join_shares_kernel<D><<<dim3(rows, a.pages.heads, a.seqs), 256, 0, stream>>>(w);
