@@ -165,7 +165,13 @@ __device__ inline void sign_channels(const int8_t *signs, int first, float (&x)[
     }
 }
 
-// The unnormalised Walsh-Hadamard butterflies of a row, the channel bits in rising order: those inside a lane, then the lane's four (DPP, as in lane_butterflies).
+// The unnormalised Walsh-Hadamard butterflies of a row, the channel bits in rising order: those inside a lane, then the lane's four, as in lane_butterflies: the partner's value
+// comes with the addition (DPP), the own one's sign is flipped before it
+template <int CTRL>
+__device__ inline float partner_of(float v)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
+}
 template <int C>
 __device__ inline void row_butterflies(float (&x)[C], int lane)
 {
@@ -178,13 +184,14 @@ __device__ inline void row_butterflies(float (&x)[C], int lane)
                 x[i] = u + v;
                 x[i | b] = u - v;
             }
-    const float s1 = (lane & 1) ? -1.0f : 1.0f, s2 = (lane & 2) ? -1.0f : 1.0f, s4 = (lane & 4) ? -1.0f : 1.0f, s8 = (lane & 8) ? -1.0f : 1.0f;
+    const uint32_t s1 = (uint32_t)lane << 31, s2 = (uint32_t)(lane >> 1) << 31, s4 = (uint32_t)(lane >> 2) << 31, s8 = (uint32_t)(lane >> 3) << 31;
+    auto flip = [](float v, uint32_t sign) { return __uint_as_float(__float_as_uint(v) ^ sign); };
 #pragma unroll
     for (int r = 0; r < C; ++r) {
-        x[r] = fmaf(x[r], s1, dpp_move<0xB1>(x[r]));
-        x[r] = fmaf(x[r], s2, dpp_move<0x4E>(x[r]));
-        x[r] = fmaf(x[r], s4, dpp_move<0x141>(dpp_move<0x1B>(x[r])));
-        x[r] = fmaf(x[r], s8, dpp_move<0x128>(x[r]));
+        x[r] = partner_of<0xB1>(x[r]) + flip(x[r], s1);
+        x[r] = partner_of<0x4E>(x[r]) + flip(x[r], s2);
+        x[r] = partner_of<0x141>(partner_of<0x1B>(x[r])) + flip(x[r], s4);
+        x[r] = partner_of<0x128>(x[r]) + flip(x[r], s8);
     }
 }
 
