@@ -1,4 +1,4 @@
-// Attention over the 4-bit key/value cache for more rows than the waves of a block share (prompts, queries on another sequence's states): a wave has 32 or 64 rows of its own and goes through all
+// Attention over the 4-bit key/value cache for more rows than the waves of a block share (prompts, queries on another sequence's states): a wave has 16, 32 or 64 rows of its own and goes through all
 // keys that they see; the four waves of a block go through the same pages at about the same time.
 #include "kv4_attention.h"
 #include "kv4_plan.h"
@@ -17,7 +17,7 @@ __device__ inline size_t partial_row(const Tiled &w, int b, int head, int row, i
 }
 
 template <int D, int NT>
-__global__ __launch_bounds__(256, (D == 64 && NT == 2 ? 3 : 2)) void kv4_own_rows_kernel(Tiled w)
+__global__ __launch_bounds__(256, (NT == 1 || (D == 64 && NT == 2) ? 3 : 2)) void kv4_own_rows_kernel(Tiled w)
 {
     constexpr int C = D / 16, kPad = D + 4;
     __shared__ __align__(16) float area[4][16 * kPad];
@@ -107,6 +107,7 @@ hipError_t launch(const Kv4Attention &a, hipStream_t stream)
     const Tiled w{a, group, p.chunk, p.splits, p.tiles, static_cast<float *>(a.workspace)};
     const dim3 grid((unsigned)a.seqs * a.pages.heads * p.tiles * p.splits);
     if (D == 64 && p.nt == 4) kv4_own_rows_kernel<64, 4><<<grid, 256, 0, stream>>>(w);
+    else if (p.nt == 1) kv4_own_rows_kernel<D, 1><<<grid, 256, 0, stream>>>(w);
     else kv4_own_rows_kernel<D, 2><<<grid, 256, 0, stream>>>(w);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
