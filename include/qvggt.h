@@ -511,6 +511,7 @@ int qvggt_calib_descent_step(float *theta, const float *grad, int n, float lr, f
  *   the pool gives wrong results for its sequence, and nothing is read outside the pool.  seqs <= 65535.  out: bf16 [T, q_heads, d]; rows of no sequence are not written.
  *   workspace: qvggt_kv4_attention_workspace_bytes of the same sizes, 16-byte aligned, NULL where that is 0.  Scores, weights and sums are fp32, queries and weights are rounded to fp16
  *   (11 bits) for the products.  Sums in a fixed order: the same call gives the same bits.
+ * T * heads at most 2^27 in qvggt_kv4_append and qvggt_kv4_read; in qvggt_kv4_attention max_kv at most 2^30 and seqs * kv_heads * ceil(max_q * (q_heads / kv_heads) / 64) at most 2^23.
  * QVGGT_ERR_SHAPE for sizes outside these limits, QVGGT_ERR_ARG for a scale that is not finite or a causal other than 0 and 1.  int32 arrays and tables need 16-byte aligned pointers as
  * everything else.
  */

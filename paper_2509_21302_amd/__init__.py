@@ -12,3 +12,4 @@ for _name in EXPORTS:
 del _name
 
 from .module import DsfqLinear  # noqa: E402,F401
+from .kv_cache import Kv4Cache  # noqa: E402,F401

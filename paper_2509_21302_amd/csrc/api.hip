@@ -2,6 +2,7 @@
 // caller's stream.  Declarations and the meaning of every argument are in include/qvggt.h.
 #include "qvggt_common.h"
 #include "kv4.h"
+#include "kv4_plan.h"
 #include "../../include/qvggt.h"
 
 #include <atomic>
@@ -860,11 +861,12 @@ qvggt::Kv4Pages pages_of(const void *cache, int num_pages, int page_tokens, int 
 {
     return {static_cast<uint8_t *>(const_cast<void *>(cache)), num_pages, __builtin_ctz((unsigned)page_tokens), heads};
 }
-bool valid_rows(int T, int heads) { return T >= 0 && (long long)T * heads <= (1LL << 33); }
+bool valid_rows(int T, int heads) { return T >= 0 && (long long)T * heads <= 1 << 27; }
 bool valid_attention(int T, int seqs, int max_q, int max_kv, int q_heads, int kv_heads, int d)
 {
     return T >= 0 && seqs >= 0 && seqs <= 65535 && max_q >= 0 && max_kv >= 0 && max_kv <= (1 << 30) && qvggt::kv4_valid_head(d) && kv_heads >= 1 && kv_heads <= 65535 &&
-           q_heads >= kv_heads && q_heads % kv_heads == 0 && (long long)max_q * (q_heads / kv_heads) <= (1 << 30);
+           q_heads >= kv_heads && q_heads % kv_heads == 0 && (long long)max_q * (q_heads / kv_heads) <= (1 << 30) &&
+           (long long)seqs * kv_heads * qvggt::kv4_div_up((long long)max_q * (q_heads / kv_heads), 64) <= qvggt::kKv4MostBlocks;
 }
 }  // namespace
 

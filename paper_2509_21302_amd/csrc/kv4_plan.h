@@ -6,6 +6,8 @@ namespace qvggt {
 
 constexpr long long kv4_div_up(long long a, long long b) { return (a + b - 1) / b; }
 
+// The most blocks of 64 rows that a call may have (a launch has less than 2^32 threads).
+constexpr long long kKv4MostBlocks = 1 << 23;
 constexpr int kKv4SharedRows = 64;          // rows of a key head (query tokens times query heads of it) up to which a block's waves share them
 
 // ---- shared rows: every block an even share of all keys
@@ -24,8 +26,9 @@ inline Kv4Shares kv4_shares(int seqs, int max_q, int max_kv, int q_heads, int kv
     const long long segments = (long long)seqs * kv_heads * p.tiles;
     while (segments * (kv4_div_up(max_kv, 1LL << p.unit_shift) + 4) >= 1LL << 30) ++p.unit_shift;
     const long long units = segments * kv4_div_up(max_kv, 1LL << p.unit_shift);
-    // Whole heads: where even the longest is not worth a join, and where the blocks are many enough to even out by themselves
-    if (max_kv <= 1024 || segments >= 4 * resident) return p;
+    // Whole heads: where even the longest is not worth a join, where the blocks are many enough to even out by themselves, and where every block would go through more lengths than
+    // it has keys' worth of time for
+    if (max_kv <= 1024 || segments >= 4 * resident || seqs > 512) return p;
     const long long blocks = kv4_div_up(units, p.least);
     p.blocks = (int)(blocks < resident ? blocks : resident);
     p.map_bytes = (size_t)kv4_div_up(4LL * (1 + seqs), 256) * 256;
@@ -54,7 +57,7 @@ inline Kv4Tiles kv4_tiles(int seqs, int max_q, int max_kv, int q_heads, int kv_h
     constexpr int kLeast = 128, kMostSplits = 32;
     double best = 0.0;
     p.splits = 0;
-    for (int n = 1; n <= kMostSplits && (n == 1 || kv4_div_up(max_kv, n) >= kLeast); ++n) {
+    for (int n = 1; n <= kMostSplits && (n == 1 || (kv4_div_up(max_kv, n) >= kLeast && blocks * n < 1 << 20)); ++n) {
         const int chunk = (int)(kv4_div_up(kv4_div_up(max_kv, n), kLeast) * kLeast);
         double turns = blocks * n / resident;
         turns = turns > 2.0 ? turns + 0.5 : (double)(int)(turns + 0.999);
