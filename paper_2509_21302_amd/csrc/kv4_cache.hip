@@ -73,8 +73,9 @@ struct Quad {
     }
 };
 
-// Keys and values of a quad's tokens.  Bound by memory where tokens are many (16411 tokens of 8 heads x 128 channels in f32, 152 MB: see the figure at the launch), by the way to the
-// position's angles and back for few.
+// Keys and values of a quad's tokens.  16411 tokens of 8 heads x 128 channels in f32, 152 MB: 44 us, 3.5 TB/s; bound by ~600 vector instructions a wave and, half of its time, by the chain
+// slots, positions, angles and rows.  Few tokens: that chain alone (one token 3.5 us with its launch).  The values' rows are read past the caches (47 us within them); the keys' are not: a
+// channel and its partner read the same row.
 template <int D, bool f32>
 __global__ __launch_bounds__(256) void kv4_append_kernel(const void *K, const void *V, int T, long long k_stride, long long v_stride, Rope rope, const int8_t *signs,
                                                          const int32_t *slots, Kv4Pages pages)
@@ -88,7 +89,7 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(const void *K, const vo
     HeadRow<C> key, value;
     key.load(k_row, f32, q.first, signs);
     key.load_turn(k_row, f32, q.first, rope, token);
-    value.load(v_row, f32, q.first, signs);
+    value.load(v_row, f32, q.first, signs, true);
     key.load_angles(q.first, rope);
     uint32_t w[2], step[2];
 #pragma unroll
@@ -122,14 +123,20 @@ __device__ inline void store_channels(void *row, bool f32, int first, const floa
 {
     if (f32) {
 #pragma unroll
-        for (int i = 0; i < C / 4; ++i) reinterpret_cast<float4 *>(static_cast<float *>(row) + first)[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+        for (int i = 0; i < C / 4; ++i) {
+            typedef float Four __attribute__((ext_vector_type(4)));
+            __builtin_nontemporal_store(Four{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]}, reinterpret_cast<Four *>(static_cast<float *>(row) + first) + i);
+        }
     } else {
+        typedef uint32_t Half __attribute__((ext_vector_type(C / 2)));
+        Half v;
 #pragma unroll
-        for (int i = 0; i < C / 4; ++i) reinterpret_cast<uint2 *>(static_cast<uint16_t *>(row) + first)[i] = make_uint2(pack_bf16x2(x[4 * i], x[4 * i + 1]), pack_bf16x2(x[4 * i + 2], x[4 * i + 3]));
+        for (int i = 0; i < C / 2; ++i) v[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+        __builtin_nontemporal_store(v, reinterpret_cast<Half *>(static_cast<uint16_t *>(row) + first));
     }
 }
 
-// What a quad's tokens hold: codes times step, turned back.
+// What a quad's tokens hold: codes times step, turned back.  Bound by memory: the same 16411 tokens into bf16, 84 MB, 23 us, 3.7 TB/s; the rows leave past the caches (24 us through them).
 template <int D>
 __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Pages pages, const int32_t *slots, int T, const int8_t *signs, bool f32, void *K, void *V)
 {
