@@ -68,8 +68,12 @@ struct Map {
     }
 };
 
-// Three waves a SIMD for 16 rows, two for 32.  Steps two and three ahead, with fewer waves for their registers, are no faster (64 sequences to 8192 keys, 128 channels, two waves: 89, 90
-// and 93 us); four waves for 64 channels leave some registers in scratch memory (48 sequences to 16384 keys, own heads: 94 us for 91).
+// Steps that a wave has ahead of it.  64 channels are half the bytes: two (one sequence of a megatoken, 16 heads: 214 us, 224 with one; 48 sequences to 16384 keys the same within the
+// runs' spread, 90.5 and 91).  128: two take the registers of a third wave (64 sequences to 8192 keys 78 us for 69).
+template <int D, int NT>
+constexpr int kAhead = D == 64 && NT == 1 ? 2 : 1;
+
+// Three waves a SIMD for 16 rows, two for 32; four for 16 rows of 64 channels leave some registers in scratch memory (48 sequences to 16384 keys, own heads: 94 us for 91).
 template <int D, int NT>
 __global__ __launch_bounds__(256, (NT == 1 ? 3 : 2)) void kv4_shared_rows_kernel(Shared w)
 {
@@ -131,7 +135,7 @@ __global__ __launch_bounds__(256, (NT == 1 ? 3 : 2)) void kv4_shared_rows_kernel
         }
         const int last = seq.len, full = visible(a, seq, row0 / w.group);
         const int t0 = (unit << w.unit_shift) + wave * 32, end = w.blocks > 0 ? min(last, (unit + part) << w.unit_shift) : last;
-        Keys<D, 1, true> keys;
+        Keys<D, kAhead<D, NT>, true> keys;
         if (last == 0) {                        // nothing is seen: zeros
             for (int row = row0 + 4 * wave + g; row < min(rows, row0 + 16 * NT); row += 16) {
                 float x[C] = {};
@@ -140,7 +144,7 @@ __global__ __launch_bounds__(256, (NT == 1 ? 3 : 2)) void kv4_shared_rows_kernel
             pos += part;
             continue;
         }
-        typedef Rows<D, NT, 1, true> Mine;
+        typedef Rows<D, NT, kAhead<D, NT>, true> Mine;
         typename Mine::Query query[NT];
 #pragma unroll
         for (int j = 0; j < NT; ++j) query[j].load(a, seq, head, w.group, row0 + 16 * j + 4 * wave + g, rows, lane);
