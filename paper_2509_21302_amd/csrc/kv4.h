@@ -56,22 +56,36 @@ struct HeadRow {
     uint32_t sign[C / 4] = {};
     int at = 0;
 
-    // once: nobody reads the row again, and the caches need not keep it
-    __device__ static void words(const void *row, bool f32, int first, uint32_t (&w)[C], bool once = false)
+    __device__ static void words(const void *row, bool f32, int first, uint32_t (&w)[C])
+    {
+        if (f32) {
+#pragma unroll
+            for (int i = 0; i < C / 4; ++i) {
+                const uint4 v = reinterpret_cast<const uint4 *>(static_cast<const float *>(row) + first)[i];
+                w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+            }
+        } else if constexpr (C == 8) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(row) + first);
+            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+        } else {
+            const uint2 v = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(row) + first);
+            w[0] = v.x; w[1] = v.y;
+        }
+    }
+    // The same of a row that nobody reads again: past the caches.
+    __device__ static void words_once(const void *row, bool f32, int first, uint32_t (&w)[C])
     {
         typedef uint32_t Four __attribute__((ext_vector_type(4)));
         typedef uint32_t Half __attribute__((ext_vector_type(C / 2)));
         if (f32) {
-            const Four *from = reinterpret_cast<const Four *>(static_cast<const float *>(row) + first);
 #pragma unroll
             for (int i = 0; i < C / 4; ++i) {
-                const Four v = once ? __builtin_nontemporal_load(from + i) : from[i];
+                const Four v = __builtin_nontemporal_load(reinterpret_cast<const Four *>(static_cast<const float *>(row) + first) + i);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) w[4 * i + k] = v[k];
             }
         } else {
-            const Half *from = reinterpret_cast<const Half *>(static_cast<const uint16_t *>(row) + first);
-            const Half v = once ? __builtin_nontemporal_load(from) : *from;
+            const Half v = __builtin_nontemporal_load(reinterpret_cast<const Half *>(static_cast<const uint16_t *>(row) + first));
 #pragma unroll
             for (int k = 0; k < C / 2; ++k) w[k] = v[k];
         }
@@ -83,7 +97,8 @@ struct HeadRow {
     }
     __device__ void load(const void *row, bool f32, int first, const int8_t *signs, bool once = false)
     {
-        words(row, f32, first, x, once);
+        if (once) words_once(row, f32, first, x);
+        else words(row, f32, first, x);
         if (signs != nullptr) {
 #pragma unroll
             for (int i = 0; i < C / 4; ++i) sign[i] = reinterpret_cast<const uint32_t *>(signs + first)[i];
