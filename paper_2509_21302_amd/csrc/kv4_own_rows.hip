@@ -1,5 +1,10 @@
 // Attention over the 4-bit key/value cache for more rows than the waves of a block share (prompts, queries on another sequence's states): a wave has 16, 32 or 64 rows of its own and goes through all
 // keys that they see; the four waves of a block go through the same pages at about the same time.
+//
+// What bounds it is the issue of vector and matrix instructions, of which the SIMD overlaps little: taking 4-bit words apart and exp2 on the one side, two products on the other (a prompt of
+// 12289 tokens, 32 heads on 8, 128 channels: 0.81 of the cycles have a vector or matrix instruction issuing, the matrix cores are busy in 0.41; 1.27 ms, 0.97 PFLOP/s of what rows see.
+// 1374 queries on 68700 keys, 16 heads x 64: 0.60 ms, 0.64 PFLOP/s).  Turning tiles of codes into fp16 numbers in LDS once a block, so that the waves share that work, is no faster
+// (64 keys at a time, or 32, one tile ahead: 1.30 to 1.58 ms): reading them back costs what it saves.
 #include "kv4_attention.h"
 #include "kv4_plan.h"
 
@@ -16,6 +21,21 @@ __device__ inline size_t partial_row(const Tiled &w, int b, int head, int row, i
     return (((size_t)b * w.a.pages.heads + head) * ((size_t)w.a.max_q * w.group) + row) * w.splits + split;
 }
 
+// The sequence with the place'th most keys, of every 64 of them: whichever order a batch has, the longest blocks begin first (448 queries on 1500 keys of 12 sequences at most, 20 heads x 64:
+// 57.7 us in reversed and in random order, 69.3 and 72.1 without).  Not where a wave has four tiles, whose registers are full (a frame over 50: 633 us for 612) and whose blocks are many
+// or of one sequence.
+__device__ inline int longest(const Kv4Attention &a, int place, int lane)
+{
+    if (a.seqs == 1) return 0;
+    const int base = place & ~63, n = min(a.seqs - base, 64), len = a.lens[base + min(lane, n - 1)];
+    int before = 0;
+    for (int i = 0; i < n; ++i) {
+        const int other = __builtin_amdgcn_readlane(len, i);
+        before += other > len || (other == len && i < lane);
+    }
+    return base + __builtin_ctzll(__builtin_amdgcn_ballot_w64(lane < n && before == place - base));     // (exactly one lane has it)
+}
+
 template <int D, int NT>
 __global__ __launch_bounds__(256, (NT == 1 || (D == 64 && NT == 2) ? 3 : 2)) void kv4_own_rows_kernel(Tiled w)
 {
@@ -26,7 +46,8 @@ __global__ __launch_bounds__(256, (NT == 1 || (D == 64 && NT == 2) ? 3 : 2)) voi
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
     // Heads first, parts next, then tiles from the last one on, where rows see most, sequences last: blocks that run together have keys in common (those of a head on one of the eight
     // dies, where heads are a multiple of eight), and a sequence's longest blocks begin first
-    const int head = blockIdx.x % a.pages.heads, rest = blockIdx.x / a.pages.heads, b = rest / (w.tiles * w.splits), place = rest % (w.tiles * w.splits);
+    const int head = blockIdx.x % a.pages.heads, rest = blockIdx.x / a.pages.heads, place = rest % (w.tiles * w.splits);
+    const int b = NT == 4 ? rest / (w.tiles * w.splits) : longest(a, rest / (w.tiles * w.splits), lane);
     const Sequence seq = sequence_of(a, b);
     const int rows = seq.n * w.group, tile = (rows + 64 * NT - 1) / (64 * NT) - 1 - place / w.splits, split = place % w.splits;
     const int row0 = (tile * 4 + wave) * 16 * NT, here = min(rows - row0, 16 * NT);

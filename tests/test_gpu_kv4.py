@@ -373,3 +373,13 @@ def test_refusals_leave_the_outputs_alone():
         q.qvggt_kv4_append(out.transpose(0, 1), out, None, good, p.args["cache"], 16)
     torch.cuda.synchronize()
     assert bool((out == 3.0).all())
+
+
+@pytest.mark.parametrize("d,kv_heads,group,causal", [(64, 2, 1, False), (128, 1, 3, True)])
+def test_attention_of_sequences_in_any_order_of_their_lengths(d, kv_heads, group, causal):
+    """More sequences than a wave has lanes, lengths that rise, fall, repeat and are zero: every sequence gets its own rows, and those alone."""
+    rng = np.random.default_rng(d)
+    kv_lens = [0, 0, 40, 40, 40] + list(range(1, 31)) + list(range(90, 60, -1)) + [int(n) for n in rng.integers(0, 60, 5)]
+    q_lens = [72 // group] + [int(n) for n in rng.integers(0, 4, len(kv_lens) - 1)]
+    assert len(kv_lens) == 70
+    Problem(d, d, 16, kv_heads * group, kv_heads, q_lens, kv_lens, causal=causal).check()
