@@ -254,6 +254,11 @@ if _raw_stream is None or _device is None:
         return None         # the current one
 
 
+def capturing(t) -> bool:
+    """Whether calls on a tensor's device are being recorded into a graph, which keeps the addresses that they are given."""
+    return t.is_cuda and torch.cuda.is_current_stream_capturing()
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
         return _raw_stream(_device()) or None

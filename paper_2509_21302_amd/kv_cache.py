@@ -16,7 +16,8 @@ class Kv4Cache:
     """num_pages pages of page_tokens tokens (a power of two, 16 .. 1024) of `heads` key/value heads of head_dim (64 or 128) channels.
 
     signs: int8 [head_dim] of +-1, or None; rope: f32 [rows, rope_dim] cosines and sines by position, or None, with rope_pair the distance of the channels that turn together
-    (include/qvggt.h).  A cache keeps one workspace, as a layer does: attend() calls of one cache follow each other on one stream, from one thread at a time.
+    (include/qvggt.h).  A cache keeps one workspace, as a layer does: attend() calls of one cache follow each other on one stream, from one thread at a time.  A larger call replaces it; one
+    that a captured call was given stays the cache's, since every replay writes into it.
     """
 
     def __init__(self, num_pages: int, page_tokens: int, heads: int, head_dim: int, signs: Optional[torch.Tensor] = None, rope: Optional[torch.Tensor] = None, rope_pair: int = 0,
@@ -28,6 +29,7 @@ class Kv4Cache:
         self.signs, self.rope, self.rope_pair = signs, rope, rope_pair
         self.pages = torch.empty(num_pages, size, dtype=torch.uint8, device=device)
         self._ws = None
+        self._captured = []         # workspaces that captured calls write into
 
     def append(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, positions: Optional[torch.Tensor] = None) -> None:
         """Keys (turned by their positions) and values [T, heads, head_dim] into slots int32 [T]: page * page_tokens + offset; -1 leaves a token out."""
@@ -41,6 +43,8 @@ class Kv4Cache:
         ws = self._ws
         if need and (ws is None or ws.numel() < need):
             ws = self._ws = torch.empty(need, dtype=torch.uint8, device=queries.device)
+        if need and q.capturing(queries) and not any(ws is kept for kept in self._captured):
+            self._captured.append(ws)
         if out is None:
             out = torch.empty(T, heads, d, dtype=torch.bfloat16, device=queries.device)
         q.qvggt_kv4_attention(queries, self.signs, 1 / math.sqrt(d) if scale is None else float(scale), causal, self.pages, self.page_tokens, self.heads, page_table, q_starts, kv_lens,
