@@ -27,7 +27,7 @@ class DsfqLinear:
     4096 are multiplied with.  Other rows of a 4-bit layer take Wf only while Wq is the tensor, and as it was, when Wf was made of it; other codes
     assigned to Wq or written into it are the ones that count.  A layer keeps one workspace, into which a call's first kernel
     writes what its second reads: calls of one layer follow each other on one stream, from one thread at a time; several streams or threads
-    take a layer each.
+    take a layer each.  More rows than before replace it; one that a captured call was given stays the layer's, since every replay writes into it.
     """
 
     def __init__(self, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, signs: Optional[torch.Tensor] = None,
@@ -92,6 +92,7 @@ class DsfqLinear:
             self._blocks_of = (self.Wq, self.Wq._version)
         self._ws = (-1, None)       # rows the workspace is large enough for, the workspace
 
+    _captured = ()                  # workspaces that captured calls write into
     _blocks_of = None               # the packed codes that Wf was made of, and their version (layers of earlier builds: not known)
 
     def _blocks_hold(self) -> bool:
@@ -100,6 +101,7 @@ class DsfqLinear:
 
     def __getstate__(self):         # a copy's tensors count their versions anew
         state = dict(self.__dict__)
+        state.pop("_captured", None)                     # (captured calls are the original's)
         if "_blocks_of" in state:
             state["_blocks_of"] = self._blocks_hold()
         return state
@@ -152,6 +154,8 @@ class DsfqLinear:
         rows, ws = self._ws         # as _workspace does
         if M > rows or ws.get_device() != X.get_device():
             ws = self._workspace(M, X.device)
+        if q.capturing(X) and not any(ws is kept for kept in self._captured):
+            self._captured += (ws,)
         Y = q.native_linear(kind, X, self.signs, self.inv_smooth, self.gelu_table, W, self.w_scale, self.bias, out, ws, self.N, bits)
         if Y is not None:
             return Y
