@@ -61,3 +61,27 @@ def test_values_that_are_no_numbers_where_rows_do_not_see_them(name):
     p, sizes = problem(name, v_scale=at_the_end(KERNELS[name][5], (1, 3), np.nan))
     none = check(p, sizes)
     assert none.any() and not none.all()
+
+
+@pytest.mark.parametrize("place", [(1, 3), (30,)])
+@pytest.mark.parametrize("name", KERNELS)
+def test_keys_that_are_no_numbers(name, place):
+    """The same of keys: rows that see one are no numbers, the others as ever."""
+    p, sizes = problem(name, k_scale=at_the_end(KERNELS[name][5], place, np.nan))
+    none = check(p, sizes)
+    assert none.any() and not none.all()
+
+
+@pytest.mark.parametrize("which", ["k_scale", "v_scale"])
+@pytest.mark.parametrize("name", KERNELS)
+def test_rows_that_see_everything(name, which):
+    p, sizes = problem(name, causal=False, **{which: at_the_end(KERNELS[name][5], (20,), np.nan)})
+    none = check(p, sizes)
+    assert none.any() and not none.all()
+
+
+@pytest.mark.parametrize("name", KERNELS)
+def test_keys_of_all_sizes(name):
+    """Steps from 0 to 2^8 of the ordinary one: a score's error grows with the score (2^-12 of the terms of its product), so the weights are those of scores up to some tens."""
+    p, sizes = problem(name, loud=2.0 ** -7, k_scale=lambda t: np.where(t % 5 == 0, 0.0, 2.0 ** (t % 9)))
+    check(p, sizes)
