@@ -210,7 +210,7 @@ struct Rows {
         }
         top = max_over_64_lanes(top);
         // 2^(13 - e) with 2^e <= top < 2^(e + 1): the largest query number of the tile in 2^13 .. 2^14, the others to an absolute error that is 2^-25 of a score unit at least.
-        // Numbers over 2^17 (scores in the ten thousands at least: one key takes all the weight) become the largest fp16 and leave the other rows alone
+        // Numbers over 2^19 (scores in the hundred thousands at least: one key takes all the weight) become the largest fp16 and leave the other rows alone; infinities and no numbers stay
         const int e = min(max((int)(__float_as_uint(top) >> 23), 127 - 11), 127 + 16);
         exponent[j] = e - 127 - 13;
         const float up = __uint_as_float((uint32_t)(127 + 13 - (e - 127)) << 23);
@@ -220,7 +220,7 @@ struct Rows {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 y[i] = x[8 * s + i] * up;
-                if (fabsf(y[i]) > 65504.0f) y[i] = copysignf(65504.0f, y[i]);
+                y[i] = fabsf(y[i]) < INFINITY ? __builtin_amdgcn_fmed3f(y[i], -65504.0f, 65504.0f) : y[i];
                 if (i & 1) y[i] *= 0.0625f;
             }
             constexpr int order[8] = {0, 4, 1, 5, 2, 6, 3, 7};

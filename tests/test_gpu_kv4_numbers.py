@@ -85,3 +85,18 @@ def test_keys_of_all_sizes(name):
     """Steps from 0 to 2^8 of the ordinary one: a score's error grows with the score (2^-12 of the terms of its product), so the weights are those of scores up to some tens."""
     p, sizes = problem(name, loud=2.0 ** -7, k_scale=lambda t: np.where(t % 5 == 0, 0.0, 2.0 ** (t % 9)))
     check(p, sizes)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("value", [np.inf, -np.inf, np.nan])
+@pytest.mark.parametrize("name", KERNELS)
+def test_queries_that_are_no_numbers(name, value, dtype):
+    """One head of one token: its row is no number, its neighbours in the same tile are as ever."""
+    p, sizes = problem(name, dtype=dtype)
+    token = p.q_lens[0] // 2
+    p.qd[token, -1, 7] = value
+    got, want = p.run(**sizes).float().cpu().numpy().astype(np.float64), p.want()
+    assert np.isnan(got[token, -1]).all()
+    got[token, -1] = want[token, -1] = 0
+    assert np.isfinite(got).all() and rel(got, want) <= BAR
+    assert (np.linalg.norm(got - want, axis=-1) <= 3 * BAR * (np.linalg.norm(want, axis=-1) + 0.05)).all()
