@@ -482,7 +482,8 @@ int qvggt_calib_descent_step(float *theta, const float *grad, int n, float lr, f
  * tokens or frames.  The quantizer is the one of the linear layer (Sec. 3.2: random signs, Hadamard rotation, symmetric 4-bit codes with a step per token), applied to
  * every head of a token: with d channels, signs s, the orthonormal Sylvester-Hadamard matrix H of d channels,
  *     z = (s * x) H,   step = bf16_rne(max_j |z_j| / 7),   code_j = rne(z_j / step) in [-7, 7],      and x is kept as   x^ = s * ((step * code) H).
- * A row of zeros, or one whose step would lie below 2^-126, has step 0 and codes 0.
+ * A row of zeros, or one whose step would lie below 2^-126, has step 0 and codes 0.  A row that has an infinity or a NaN, or whose sums overflow fp32, has a step that is NaN and codes 0: it
+ * reads back as NaN, and attention gives NaN to the rows that see it, and only to those.
  *
  * Pages.  d = 64 or 128 channels; a page holds page_tokens tokens (a power of two, 16 .. 1024) of all `heads` key/value heads in
  * qvggt_kv4_page_bytes(page_tokens, heads, d) = heads * page_tokens * (d + 4) bytes (0 for unsupported sizes); a pool of num_pages of them is one buffer, `cache`, of
@@ -504,7 +505,8 @@ int qvggt_calib_descent_step(float *theta, const float *grad, int n, float lr, f
  * qvggt_kv4_attention:  for every sequence b, its n = q_starts[b + 1] - q_starts[b] query tokens (rows q_starts[b] .. of Q) over its first len = kv_lens[b] keys and values, which lie
  *   in the pages page_table[b, 0], page_table[b, 1], ...:
  *     out[i, h, :] = sum_j softmax_j( scale * <rotated q[i, h], k^[j, h']> ) v^[j, h'],     h' = h / (q_heads / kv_heads),
- *   j over the keys 0 .. len - n + i with causal = 1 (the queries are the sequence's last n tokens), 0 .. len - 1 with causal = 0.  A query that sees no key gives zeros.
+ *   j over the keys 0 .. len - n + i with causal = 1 (the queries are the sequence's last n tokens), 0 .. len - 1 with causal = 0.  A query that sees no key gives zeros,
+ *   one that is no number (an infinity or a NaN in its head) NaN.
  *   Q: bf16 or f32 [T, q_heads, d], token t at q_stride * t elements.  q_heads a multiple of kv_heads.  signs as given to qvggt_kv4_append.  q_starts: int32 [seqs + 1], not falling;
  *   kv_lens: int32 [seqs]; page_table: int32 [seqs, table_width].  max_q and max_kv: at least every n and len (they decide how the work is cut up; longer sequences are cut off at them),
  *   max_kv <= table_width * page_tokens.  What lies in pages behind a sequence's end, and entries of page_table behind its last page, may be anything.  An entry in use that is no page of

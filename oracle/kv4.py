@@ -36,9 +36,12 @@ def bf16_rne(x):
 
 
 def quantize(x, signs):
-    """(codes int, steps) of x [..., d]: z = (s x) H, step = bf16(max |z| / 7), rne(z / step)."""
-    z = (x * signs) @ hadamard(x.shape[-1])
-    step = bf16_rne(np.abs(z).max(-1) / 7)
+    """(codes int, steps) of x [..., d]: z = (s x) H, step = bf16(max |z| / 7), rne(z / step); step NaN and codes 0 where z is not finite."""
+    with np.errstate(invalid="ignore"):
+        z = (x * signs) @ hadamard(x.shape[-1])
+    finite = np.isfinite(z).all(-1)
+    z = np.where(finite[..., None], z, 0.0)
+    step = np.where(finite, bf16_rne(np.abs(z).max(-1) / 7), np.nan)
     step = np.where(step < 2.0 ** -126, 0.0, step)
     codes = np.rint(np.divide(z, step[..., None], out=np.zeros_like(z), where=step[..., None] > 0)).clip(-8, 7)
     return codes.astype(np.int64), step

@@ -23,22 +23,23 @@ __device__ inline uint32_t nibbles(const float (&z)[C], float step, float inv)
     return w;
 }
 
-// z -> its step, rounded to bf16 (8 bits of a step that is uncertain by half a code: the codes are taken with the rounded step, so nothing else changes), and the codes
+// z -> its step, rounded to bf16 (8 bits of a step that is uncertain by half a code: the codes are taken with the rounded step, so nothing else changes), and the codes.  A row with an
+// infinity or no number in it, or whose sums overflow, has a step that is none: maxima here pass that on, and all that is read of the row shows it
 template <int C>
 __device__ inline uint32_t quantize(float (&z)[C], uint32_t *step_bits)
 {
     float top = 0.0f;
 #pragma unroll
-    for (int i = 0; i < C; ++i) top = fmaxf(top, fabsf(z[i]));
-    top = fmaxf(top, partner_of<0xB1>(top));            // over the row's 16 lanes, as max_over_16_lanes
-    top = fmaxf(top, partner_of<0x4E>(top));
-    top = fmaxf(top, partner_of<0x141>(top));
-    top = fmaxf(top, partner_of<0x140>(top));
+    for (int i = 0; i < C; ++i) top = __builtin_elementwise_maximum(top, fabsf(z[i]));
+    top = __builtin_elementwise_maximum(top, partner_of<0xB1>(top));            // over the row's 16 lanes, as max_over_16_lanes
+    top = __builtin_elementwise_maximum(top, partner_of<0x4E>(top));
+    top = __builtin_elementwise_maximum(top, partner_of<0x141>(top));
+    top = __builtin_elementwise_maximum(top, partner_of<0x140>(top));
     const uint32_t bits = pack_bf16x2(top / 7.0f, 0.0f) & 0xffffu;
     const float step = bf16_bits_to_float(bits);
-    const bool live = step >= kMinStep;
-    *step_bits = live ? bits : 0;
-    return nibbles<C>(z, step, live ? 1.0f / step : 0.0f);
+    const bool number = top < INFINITY, live = number && step >= kMinStep;
+    *step_bits = live ? bits : number ? 0 : 0x7fc0u;
+    return live ? nibbles<C>(z, step, 1.0f / step) : 0x88888888u >> (32 - 4 * C);
 }
 
 // Four tokens' bytes of values, a token in each of the lanes n, n + 16, n + 32, n + 48, become words of a pair of channels: lane n + 16 i then has byte i of all four.  Its own inverse.

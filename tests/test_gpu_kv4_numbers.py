@@ -2,9 +2,11 @@
 what it sees and is no number must show.  Bars as in test_gpu_kv4.py."""
 import numpy as np
 import pytest
+import torch
 
+import paper_2509_21302_amd as q
 from oracle import kv4
-from tests.test_gpu_kv4 import BAR, Problem, rel
+from tests.test_gpu_kv4 import BAR, DEV, Problem, dev, rel, signs_of, table_of
 
 pytestmark = pytest.mark.gpu
 # sizes and stated sizes (max_q, max_kv) that take each kernel: shared rows of one and two tiles, whole and in shares; own rows of one, two and four tiles, whole and in parts
@@ -100,3 +102,46 @@ def test_queries_that_are_no_numbers(name, value, dtype):
     got[token, -1] = want[token, -1] = 0
     assert np.isfinite(got).all() and rel(got, want) <= BAR
     assert (np.linalg.norm(got - want, axis=-1) <= 3 * BAR * (np.linalg.norm(want, axis=-1) + 0.05)).all()
+
+
+@pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf, 3e38])
+@pytest.mark.parametrize("d,page,heads,T,pair,dtype,scattered", [(64, 16, 2, 41, 16, torch.bfloat16, False), (128, 32, 3, 41, 64, torch.float32, False),
+                                                                 (64, 32, 3, 37, 0, torch.float32, True), (128, 16, 2, 37, 1, torch.bfloat16, True)])
+def test_append_of_rows_that_are_no_numbers(d, page, heads, T, pair, dtype, scattered, value):
+    """A key's head in one token and a value's in another (a number so large that 64 of them overflow, too): steps that are NaN and codes 0 there, every other byte as without them."""
+    rng = np.random.default_rng(T)
+    x = torch.from_numpy(rng.standard_normal((T, 2 * heads, d))).to(dtype)
+    bad = x.clone()
+    everywhere = slice(None) if value == 3e38 else slice(5, 6)
+    bad[9, 1, everywhere], bad[20, heads, everywhere] = value, value
+    if value == 3e38:
+        signs, pair = None, 0                                # equal numbers add up in the first channel
+    else:
+        signs = dev(signs_of(rng, d))
+    table, positions = dev(table_of(rng, 50, d if pair else 0)), dev(rng.integers(0, 50, T).astype(np.int32))
+    slots = rng.permutation(6 * page)[:T] if scattered else 3 + np.arange(T)
+    where = dev(slots.astype(np.int32))
+    pools = []
+    for rows in (x, bad):
+        pools.append(torch.zeros(6, q.qvggt_kv4_page_bytes(page, heads, d), dtype=torch.uint8, device=DEV))
+        rows = rows.to(DEV)
+        q.qvggt_kv4_append(rows[:, :heads], rows[:, heads:], signs, where, pools[-1], page, rope=table, positions=positions, rope_pair=pair)
+    want = pools[0].cpu().numpy().ravel()
+    for t, head, which in ((9, 1, 0), (20, 0, 1)):
+        kv4.store(want, page, heads, d, int(slots[t]), head, which, np.zeros(d, int), np.float32(np.nan))
+    assert np.array_equal(pools[1].cpu().numpy().ravel(), want)
+    K, V = (torch.zeros(T, heads, d, device=DEV) for _ in range(2))
+    q.qvggt_kv4_read(pools[1], page, signs, where, K, V)
+    for out, t, head in ((K, 9, 1), (V, 20, 0)):
+        assert bool(out[t, head].isnan().all()) and int(out.isnan().sum()) == d
+    # rows that see them: head 1 from token 9 on, head 0 from token 20 on
+    if not scattered and value != 3e38:
+        table_of_pages = torch.arange(6, device=DEV, dtype=torch.int32)[None]
+        starts, lens = dev(np.array([0, T], np.int32)), dev(np.array([T + 3], np.int32))
+        queries = torch.randn(T, heads, d, device=DEV)
+        out = torch.zeros(T, heads, d, dtype=torch.bfloat16, device=DEV)
+        q.qvggt_kv4_attention(queries, signs, 0.1, True, pools[1], page, heads, table_of_pages, starts, lens, T, T + 3, out, None)
+        first = torch.full((heads,), T)
+        first[1], first[0] = 9, 20
+        none = torch.arange(T)[:, None] >= first[None]
+        assert torch.equal(out.isnan().all(2).cpu(), none) and torch.equal(out.isnan().any(2).cpu(), none)
