@@ -320,6 +320,21 @@ struct Rows {
             p.w[2 * h + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(w[1], w[3]));
         }
     }
+    // The offset of 8 out of the sums so far.  It grows with every key, what is left of the sums without it (values of both signs) much less, and every addition is rounded at the size of the
+    // whole: over 2^20 keys of the same weight in one wave 1.7 % of the result, and below 10^-4 where the offset starts anew every kFold steps
+    static constexpr int kFold = 256;
+    __device__ void fold()
+    {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                acc[j][2 * w] -= ones[j];
+                acc[j][2 * w + 1] -= 16.0f * ones[j];
+            }
+            ones[j] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+    }
     // The 32 keys from t0, which `x` holds in place d, and the fetch of those AHEAD steps on.  EDGE: some row does not see all of them; last: keys that some row sees.
     template <bool EDGE>
     __device__ void take(Keys<D, AHEAD, ONCE> &x, int d, int t0, int stride, int last, int g)
@@ -409,6 +424,7 @@ struct Rows {
         for (const int whole = min(full, stop) - 32 - (AHEAD - 1) * stride; t0 <= whole; t0 += AHEAD * stride) {
 #pragma unroll
             for (int d = 0; d < AHEAD; ++d) take<false>(x, d, t0 + d * stride, stride, last, g);
+            if ((t0 & (kFold * stride - 1)) < AHEAD * stride) fold();        // (stride is a power of two: once in kFold steps, wherever they began)
         }
         for (; t0 < stop; t0 += AHEAD * stride) {
 #pragma unroll

@@ -55,6 +55,9 @@ inline Kv4Tiles kv4_tiles(int seqs, int max_q, int max_kv, int q_heads, int kv_h
     const double blocks = (double)p.tiles * pairs;
     // How many parts: turns of the resident blocks times a part's keys and what a block costs besides, and the partial sums to memory and back; in units of a key's 40 ns
     constexpr int kLeast = 128, kMostSplits = 32;
+    // A part has 2^20 keys at most as long as there may be more of them: a wave adds its keys' weights and values up in fp32, two additions every 32 keys, and the last bit of a sum of 2^16
+    // terms is within 2^-9 of it in the worst case, in which every addition is rounded the same way
+    constexpr int kMostKeys = 1 << 20;
     double best = 0.0;
     p.splits = 0;
     for (int n = 1; n <= kMostSplits && (n == 1 || (kv4_div_up(max_kv, n) >= kLeast && blocks * n < 1 << 20)); ++n) {
@@ -63,7 +66,7 @@ inline Kv4Tiles kv4_tiles(int seqs, int max_q, int max_kv, int q_heads, int kv_h
         turns = turns > 2.0 ? turns + 0.5 : (double)(int)(turns + 0.999);
         const double join = n == 1 ? 0.0 : 200.0 + (double)pairs * rows * n * (d + 2) * 8 / 4.5e6 / 0.04;
         const double cost = turns * (chunk + 300) + join;
-        if (p.splits == 0 || cost < best) {
+        if (p.splits == 0 || cost < best || p.chunk > kMostKeys) {
             best = cost;
             p.chunk = chunk < kLeast ? kLeast : chunk;
             p.splits = n;
@@ -72,7 +75,7 @@ inline Kv4Tiles kv4_tiles(int seqs, int max_q, int max_kv, int q_heads, int kv_h
     // One tile a wave: blocks of 64 rows that take 0.7 or 0.75 of the time while there are few of them, whole sequences only, where that is less (a prompt of 512 tokens, 32 heads on 8:
     // 17 us for 24 with 64 channels, 22 for 31 with 128; but a prompt of 12289 tokens 1.61 ms for 1.29)
     const double short_turns = (double)(kv4_div_up(rows, 64) * pairs) / (256 * 3);
-    if (short_turns <= 3.0 && (short_turns > 2.0 ? short_turns + 0.5 : (double)(int)(short_turns + 0.999)) * (max_kv + 300) * (d == 64 ? 0.75 : 0.7) < best) {
+    if (max_kv <= kMostKeys && short_turns <= 3.0 && (short_turns > 2.0 ? short_turns + 0.5 : (double)(int)(short_turns + 0.999)) * (max_kv + 300) * (d == 64 ? 0.75 : 0.7) < best) {
         p.nt = 1;
         p.tiles = (int)kv4_div_up(rows, 64);
         p.chunk = max_kv < kLeast ? kLeast : max_kv;
