@@ -37,18 +37,21 @@ constexpr int kSmallest = -90;                  // log2 of the least largest ste
 
 // what a block knows about its sequence
 struct Sequence {
-    int start, n, len;
+    int start, n, len;      // queries and keys, cut off at what the caller states as their most
+    int before;             // keys in front of the first query's own, of the whole sequence (or the most keys, where there are more): what is cut off must not shift what a query sees
 };
 __device__ inline Sequence sequence_of(const Kv4Attention &a, int b)
 {
     Sequence s;
     s.start = min(max(a.starts[b], 0), a.T);
-    s.n = min(min(max(a.starts[b + 1] - s.start, 0), a.max_q), a.T - s.start);
-    s.len = min(max(a.lens[b], 0), a.max_kv);
+    const int n = max(min(a.starts[b + 1], a.T) - s.start, 0), len = max(a.lens[b], 0);
+    s.n = min(n, a.max_q);
+    s.len = min(len, a.max_kv);
+    s.before = min(len - n, a.max_kv);
     return s;
 }
 // keys that a query token sees
-__device__ inline int visible(const Kv4Attention &a, const Sequence &s, int token) { return a.causal ? min(max(s.len - s.n + token + 1, 0), s.len) : s.len; }
+__device__ inline int visible(const Kv4Attention &a, const Sequence &s, int token) { return a.causal ? min(max(s.before + token + 1, 0), s.len) : s.len; }
 
 // floats of a row's partial sums: D sums, the maximum, the sum of weights
 template <int D>

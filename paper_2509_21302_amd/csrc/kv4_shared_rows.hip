@@ -32,7 +32,7 @@ __device__ inline int cost_of(const Shared &w, const Sequence &s)
 // Where a unit number lies, 64 sequences at a time.  A wave keeps them in its own part of LDS (in registers they would be beside the sums).
 struct Map {
     struct Place {
-        int upto[64], start[64], n[64], len[64];        // cost of a head of the sequences up to and with this one; the sequence
+        int upto[64], start[64], n[64], len[64], before[64];        // cost of a head of the sequences up to and with this one; the sequence
     };
     Place *place;
     int base, before, total;            // sequences and cost before the 64; cost up to their end
@@ -52,6 +52,7 @@ struct Map {
         place->start[lane] = s.start;
         place->n[lane] = s.n;
         place->len[lane] = s.len;
+        place->before[lane] = s.before;
         lanes_exchange_fence();
         total = before + __builtin_amdgcn_readlane(scan, 63);
     }
@@ -65,7 +66,8 @@ struct Map {
     }
     __device__ Sequence sequence(int in) const
     {
-        return {__builtin_amdgcn_readfirstlane(place->start[in]), __builtin_amdgcn_readfirstlane(place->n[in]), __builtin_amdgcn_readfirstlane(place->len[in])};
+        return {__builtin_amdgcn_readfirstlane(place->start[in]), __builtin_amdgcn_readfirstlane(place->n[in]), __builtin_amdgcn_readfirstlane(place->len[in]),
+                __builtin_amdgcn_readfirstlane(place->before[in])};
     }
 };
 
