@@ -145,3 +145,13 @@ def test_append_of_rows_that_are_no_numbers(d, page, heads, T, pair, dtype, scat
         first[1], first[0] = 9, 20
         none = torch.arange(T)[:, None] >= first[None]
         assert torch.equal(out.isnan().all(2).cpu(), none) and torch.equal(out.isnan().any(2).cpu(), none)
+
+
+@pytest.mark.parametrize("d,heads,kv_heads,q_lens,kv_lens", [(128, 16, 2, [1] * 32, [300] * 32), (64, 8, 2, [4] * 32, [250] * 32), (64, 2, 2, [300], [400]), (128, 2, 1, [256], [300])])
+def test_results_are_not_too_small(d, heads, kv_heads, q_lens, kv_lens):
+    """Every rounding is to nearest, so errors do not add up to a factor: what results are along the right ones.  512 rows or more of 64 or 128 values, each over hundreds of keys of like
+    weight: the rounding to bf16 is 8e-4 of a value rms, 8e-4 sqrt(3 / 32768) = 8e-6 along all of them; a weight's to fp16 1.4e-4, 1.4e-4 / sqrt(50 * 512) = 1e-6.  The bar is five times
+    both.  Weights cut off at fp16's last bit would take 2^-12 or more."""
+    p = Problem(len(q_lens), d, 16, heads, kv_heads, q_lens, kv_lens, causal=False)
+    got, want = p.run().double().cpu().numpy().ravel(), p.want().ravel()
+    assert abs((got @ want) / (want @ want) - 1) <= 5e-5
