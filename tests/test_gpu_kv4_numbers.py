@@ -8,7 +8,6 @@ import paper_2509_21302_amd as q
 from oracle import kv4
 from tests.test_gpu_kv4 import BAR, DEV, Problem, dev, rel, signs_of, table_of
 
-pytestmark = pytest.mark.gpu
 # sizes and stated sizes (max_q, max_kv) that take each kernel: shared rows of one and two tiles, whole and in shares; own rows of one, two and four tiles, whole and in parts
 KERNELS = {
     "shared": (128, 16, 4, 2, [5, 1], [60, 33], 5, 100), "shared_64": (64, 16, 2, 2, [9, 3], [60, 20], 9, 100), "shared_two_tiles": (64, 16, 2, 1, [30, 17], [60, 64], 30, 100),
@@ -57,6 +56,7 @@ def at_the_end(p, places, value):
     return lambda t: np.where((len(t) == n) & np.isin(n - t, places), value, 1.0)
 
 
+@pytest.mark.gpu
 @pytest.mark.parametrize("name", KERNELS)
 def test_values_that_are_no_numbers_where_rows_do_not_see_them(name):
     """A step that is no number, as qvggt_kv4_append leaves it for a row that has an infinity or a NaN, in two values near the end: rows in front of them have none of it."""
@@ -65,6 +65,7 @@ def test_values_that_are_no_numbers_where_rows_do_not_see_them(name):
     assert none.any() and not none.all()
 
 
+@pytest.mark.gpu
 @pytest.mark.parametrize("place", [(1, 3), (30,)])
 @pytest.mark.parametrize("name", KERNELS)
 def test_keys_that_are_no_numbers(name, place):
@@ -74,6 +75,7 @@ def test_keys_that_are_no_numbers(name, place):
     assert none.any() and not none.all()
 
 
+@pytest.mark.gpu
 @pytest.mark.parametrize("which", ["k_scale", "v_scale"])
 @pytest.mark.parametrize("name", KERNELS)
 def test_rows_that_see_everything(name, which):
@@ -82,6 +84,7 @@ def test_rows_that_see_everything(name, which):
     assert none.any() and not none.all()
 
 
+@pytest.mark.gpu
 @pytest.mark.parametrize("name", KERNELS)
 def test_keys_of_all_sizes(name):
     """Steps from 0 to 2^8 of the ordinary one: a score's error grows with the score (2^-12 of the terms of its product), so the weights are those of scores up to some tens."""
@@ -89,6 +92,7 @@ def test_keys_of_all_sizes(name):
     check(p, sizes)
 
 
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("value", [np.inf, -np.inf, np.nan])
 @pytest.mark.parametrize("name", KERNELS)
@@ -104,6 +108,7 @@ def test_queries_that_are_no_numbers(name, value, dtype):
     assert (np.linalg.norm(got - want, axis=-1) <= 3 * BAR * (np.linalg.norm(want, axis=-1) + 0.05)).all()
 
 
+@pytest.mark.gpu
 @pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf, 3e38])
 @pytest.mark.parametrize("d,page,heads,T,pair,dtype,scattered", [(64, 16, 2, 41, 16, torch.bfloat16, False), (128, 32, 3, 41, 64, torch.float32, False),
                                                                  (64, 32, 3, 37, 0, torch.float32, True), (128, 16, 2, 37, 1, torch.bfloat16, True)])
@@ -147,6 +152,7 @@ def test_append_of_rows_that_are_no_numbers(d, page, heads, T, pair, dtype, scat
         assert torch.equal(out.isnan().all(2).cpu(), none) and torch.equal(out.isnan().any(2).cpu(), none)
 
 
+@pytest.mark.gpu
 @pytest.mark.parametrize("d,heads,kv_heads,q_lens,kv_lens", [(128, 16, 2, [1] * 32, [300] * 32), (64, 8, 2, [4] * 32, [250] * 32), (64, 2, 2, [300], [400]), (128, 2, 1, [256], [300])])
 def test_results_are_not_too_small(d, heads, kv_heads, q_lens, kv_lens):
     """Every rounding is to nearest, so errors do not add up to a factor: what results are along the right ones.  512 rows or more of 64 or 128 values, each over hundreds of keys of like
@@ -155,3 +161,66 @@ def test_results_are_not_too_small(d, heads, kv_heads, q_lens, kv_lens):
     p = Problem(len(q_lens), d, 16, heads, kv_heads, q_lens, kv_lens, causal=False)
     got, want = p.run().double().cpu().numpy().ravel(), p.want().ravel()
     assert abs((got @ want) / (want @ want) - 1) <= 5e-5
+
+
+def sharp_bound(turned, keys, values, scale):
+    """(the result of one row, how far off each of its channels may be); turned and keys in the turned basis, where products are taken.  A channel of the query is an fp16 number, off by 2^-11
+    of itself at most, so score j is off by D_j = 2^-11 times the sum of the magnitudes of its product's terms.  With o the result, weights times e^+-D_j change it by
+    sum_j p_j (e^D_j - 1) |v_j - o| over the new sum of weights, which is e^-max D at least.  A weight times its step is an fp16 number too, 2^-11 of it, beside a sum of weights that is
+    not: 2^-11 sum_j p_j |v_j|, with the p_j that they are by then.  The result is rounded to 8 bits: 2^-8.  These sums are of the codes, whose basis the result is turned back from: a channel gets
+    the 2-norm of such errors at most.  fp32 arithmetic: 2^-20 of the largest terms."""
+    score = scale * keys @ turned
+    weight = np.exp(score - score.max())
+    weight /= weight.sum()
+    o = weight @ values
+    d = 2.0 ** -11 * scale * np.abs(keys) @ np.abs(turned) + 2.0 ** -20 * np.abs(score)
+    moved = np.minimum(weight * np.exp(np.minimum(d + d.max(), 100.0)), 1.0)
+    shift = np.minimum(weight * np.expm1(np.minimum(d, 100.0)) * np.exp(min(d.max(), 100.0)), 1.0)
+    length = np.linalg.norm(values, axis=1)
+    inner = shift @ np.linalg.norm(values - o, axis=1) + 2.0 ** -11 * moved @ length + 2.0 ** -20 * length.max()
+    return o, inner + 2.0 ** -8 * (np.abs(o) + inner)
+
+
+def fp16(x):
+    return np.asarray(x, np.float16).astype(np.float64)
+
+
+@pytest.mark.parametrize("loud", [3.0, 30.0, 300.0])
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_bound_of_sharp_scores_holds_for_its_roundings(d, loud):
+    """The bound against the roundings that it is for, done here (no GPU)."""
+    rng = np.random.default_rng(d)
+    H = kv4.hadamard(d)
+    for _ in range(200):
+        n = int(rng.integers(1, 90))
+        k, v = (kv4.quantize(rng.standard_normal((n, d)), np.ones(d)) for _ in range(2))
+        keys, values = k[0] * k[1][:, None], kv4.held(*v, np.ones(d))
+        turned = loud * rng.standard_normal(d)
+        o, bound = sharp_bound(turned, keys, values, d ** -0.5)
+        up = 2.0 ** (13 - np.floor(np.log2(np.abs(turned).max())))
+        score = d ** -0.5 * keys @ fp16(turned * up) / up
+        weight = np.exp(score - score.max())
+        step = v[1] / v[1].max()
+        got = kv4.bf16_rne(fp16(weight * step * 128) @ v[0] @ H * v[1].max() / 128 / weight.sum())
+        assert (np.abs(got - o) <= bound).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("loud", [3.0, 30.0, 300.0])
+@pytest.mark.parametrize("name", KERNELS)
+def test_every_row_of_sharp_scores(name, loud):
+    """Scores of tens to thousands, every row within its own bound."""
+    p, sizes = problem(name, loud=loud)
+    got = p.run(**sizes).double().cpu().numpy()
+    H, group = kv4.hadamard(p.d), p.heads // p.kv_heads
+    signs = p.args["signs"].cpu().numpy().astype(float)
+    close = 0
+    for i, (n, k, v) in enumerate(zip(p.q_lens, p.k, p.v)):
+        for j in range(n):
+            row, seen = p.starts[i] + j, min(max(len(k) - n + j + 1, 0), len(k))
+            for h in range(p.heads if seen else 0):
+                o, bound = sharp_bound(p.turned[row, h] * signs @ H, k[:seen, h // group] * signs @ H, v[:seen, h // group], p.scale)
+                assert (np.abs(got[row, h] - o) <= bound).all(), (i, j, h)
+                close += np.linalg.norm(bound) <= 0.2 * np.linalg.norm(o)
+    if loud >= 30:
+        assert close >= 0.1 * len(p.x) * p.heads             # the bound says something of a good part of the rows
