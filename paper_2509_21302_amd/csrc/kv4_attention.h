@@ -122,8 +122,8 @@ struct Keys {
     template <int N>
     __device__ static void words(const uint8_t *base, uint32_t offset, uint32_t (&w)[N])
     {
-        // 64 channels: the offset beside an address in scalar registers.  Left alone, the compiler keeps it as 64 bits across the loop and adds them, six registers more: two tiles would spill
-        // (128 channels have the room, and the additions are free: a prompt of 12289 tokens 1.32 ms, 1.34 this way)
+        // 64 channels: the offset beside an address in scalar registers.  Left alone, the compiler keeps it as 64 bits across the loop and adds them, six registers more, and four tiles spill
+        // (a frame over 50: 620 us, 643 without).  128 channels have the room, and the additions cost nothing there
         if (D == 64) asm("" : "+v"(offset) : "s"((uint32_t)(uintptr_t)base));
         const uint8_t *const from = base + offset;
         typedef uint32_t Vector __attribute__((ext_vector_type(N)));
@@ -432,10 +432,13 @@ struct Rows {
     // The steps t0, t0 + stride, ... below stop; the first of them are below `full`, which every row sees.  (One loop with both kinds of step in it takes 70 registers more.)
     __device__ void run(Keys<D, AHEAD, ONCE> &x, int t0, int stride, int full, int last, int stop, int g)
     {
-        for (const int whole = min(full, stop) - 32 - (AHEAD - 1) * stride; t0 <= whole; t0 += AHEAD * stride) {
+        for (const int whole = min(full, stop) - 32 - (AHEAD - 1) * stride; t0 <= whole;) {
+            const int pause = min(whole, t0 | (kFold * stride - 1));
+            for (; t0 <= pause; t0 += AHEAD * stride) {
 #pragma unroll
-            for (int d = 0; d < AHEAD; ++d) take<false>(x, d, t0 + d * stride, stride, last, g);
-            if ((t0 & (kFold * stride - 1)) < AHEAD * stride) fold();        // (stride is a power of two: once in kFold steps, wherever they began)
+                for (int d = 0; d < AHEAD; ++d) take<false>(x, d, t0 + d * stride, stride, last, g);
+            }
+            fold();                         // (a loop of its own around the steps: 2 % less than a branch within them)
         }
         for (; t0 < stop; t0 += AHEAD * stride) {
 #pragma unroll

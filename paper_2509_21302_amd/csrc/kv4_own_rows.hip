@@ -76,23 +76,19 @@ __global__ __launch_bounds__(256, (NT == 1 || (D == 64 && NT == 2) ? 3 : 2)) voi
     Keys<D, 1, false> keys;
     if (t0 < stop) keys.begin(a, b, head, last, t0, 32, lane);
     r.run(keys, t0, 32, full, last, stop, g);
-    // (128 channels: the lane's number is worked out again, and not kept in registers beside the loop; 64: it costs four tiles 4 %)
-    unsigned none = 0;
-    asm volatile("" : "+s"(none));
-    const int me = D == 64 ? lane : __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, none));
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-        r.leave(j, mine, tops[wave], totals[wave], me);
+        r.leave(j, mine, tops[wave], totals[wave], lane);
         lanes_exchange_fence();
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const int r16 = 4 * k + (me >> 4), row = row0 + 16 * j + r16, first = (me & 15) * C;
+            const int r16 = 4 * k + g, row = row0 + 16 * j + r16, first = (lane & 15) * C;
             float x[C];
 #pragma unroll
             for (int i = 0; i < C; ++i) x[i] = mine[r16 * kPad + first + i];
             if (row < rows) {
-                if (w.splits == 1) finish_row<D>(a, w.group, seq, head, row, x, totals[wave][r16], me);
-                else leave_row<D>(w.partials + partial_row(w, b, head, row, split) * kPartial<D>, x, tops[wave][r16], totals[wave][r16], me);
+                if (w.splits == 1) finish_row<D>(a, w.group, seq, head, row, x, totals[wave][r16], lane);
+                else leave_row<D>(w.partials + partial_row(w, b, head, row, split) * kPartial<D>, x, tops[wave][r16], totals[wave][r16], lane);
             }
         }
         lanes_exchange_fence();
