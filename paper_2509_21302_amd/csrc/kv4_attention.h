@@ -180,11 +180,13 @@ struct Rows {
     int end[NT];                        // keys that the lane's row sees
     int exponent[NT];                   // log2 of a tile's unit
     float unit;                         // of the product of a query number and a subnormal: 1 .. 2^27
-    // Weights are 2^(score - m): m is the running maximum less `lift`, by which weights times steps fill fp16's range (kTop below the top at a step of `reach`, a power of two that no
-    // value's step so far is above).  l: their sum; acc, ones: their sums times step times code + 8, and times step times 8.  Whatever the lift, sums over l are the result.
+    // Weights are 2^(score - m): m is the running maximum less the row's lift, by which weights times steps fill fp16's range (kTop below the top at a step that is the power of two above
+    // all steps of values that the row has seen; a row's own, so that nothing depends on values that only its neighbours see).  l: their sum; acc, ones: their sums times step times code + 8,
+    // and times step times 8.  Whatever the lift, sums over l are the result.
     float4v acc[NT][2 * W], ones[NT];
     float m[NT], l[NT];
-    float reach, lift;
+    float *lifts;                       // of the wave's rows, in LDS: [tile][row]
+    float reach, low;                   // of all rows: the least power of two, the least lift
     uint32_t seen;                      // bit j: the lane's row of tile j has a maximum (or will never have one)
     float unseen;                       // infinite until all have
 
@@ -247,8 +249,9 @@ struct Rows {
         return highest;
     }
     // all tiles on one power of two, and nothing seen yet
-    __device__ void start(int highest)
+    __device__ void start(int highest, float *room)
     {
+        lifts = room;
         unit = __uint_as_float((uint32_t)(highest + 24 + 127) << 23);
         const float4v zero = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -270,39 +273,52 @@ struct Rows {
             ones[j] = zero;
             m[j] = l[j] = 0.0f;
         }
-        reach = lift = 0.0f;
+        reach = low = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) lifts[16 * j + row_of_lane()] = kTop - kSmallest;
         seen = 0;
 #pragma unroll
         for (int j = 0; j < NT; ++j) seen |= (uint32_t)(end[j] == 0) << j;
         unseen = INFINITY;
     }
-    // t: the scores of a step above m, -inf where a row does not see a key.  Where one is above the maximum by more than the slack, a value's step above all before, or a row without
-    // a maximum: maxima and lift anew, and t and the sums with them.  (Scores are got back from t: nothing else of the step is kept for this.)
-    __device__ void raise(float (&t)[NT][2][4], float over, float tops)
+    // The lane's row of a tile, without a register of its own beside the loops
+    __device__ static int row_of_lane()
     {
-        if (!__builtin_amdgcn_ballot_w64(over > kSlack + lift || tops > reach)) return;
-        tops = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(max_over_64_lanes(tops))));        // (reach and lift stay scalar)
-        const float before = lift;
-        if (tops > reach) {
-            const int e = max((int)(__float_as_uint(tops) >> 23) - 126, kSmallest);            // 2^e > tops
-            reach = __uint_as_float((uint32_t)(min(e, 127) + 127) << 23);
-            lift = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int((float)(kTop - e))));
-        }
+        unsigned none = 0;
+        asm volatile("" : "+s"(none));
+        return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, none)) & 15;
+    }
+    // t: the scores of a step above m, -inf where a row does not see a key.  Where one is above the maximum by more than the slack, a value's step above all that some row has seen, or a row
+    // without a maximum: maxima and lifts anew, and t and the sums with them.  (Scores are got back from t: nothing else of the step is kept for this.)
+    __device__ void raise(float (&t)[NT][2][4], const float (&vs)[2][4], float over, float tops)
+    {
+        if (!__builtin_amdgcn_ballot_w64(over > kSlack + low || tops > reach)) return;
+        float lowest = kTop - kSmallest, highest = kTop - 127;
+        float *const mine = lifts + row_of_lane();
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            float top = -INFINITY;
+            float top = -INFINITY, loud = 0.0f;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) top = fmaxf(top, t[j][h][i]);
+                for (int i = 0; i < 4; ++i) {
+                    top = fmaxf(top, t[j][h][i]);
+                    loud = fmaxf(loud, t[j][h][i] > -INFINITY ? vs[h][i] : 0.0f);
+                }
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
+            loud = fmaxf(loud, __shfl_xor(loud, 16));
+            loud = fmaxf(loud, __shfl_xor(loud, 32));
+            const float before = mine[16 * j], lift = fminf(before, (float)(kTop - max((int)(__float_as_uint(loud) >> 23) - 126, kSmallest)));          // (2^(kTop - lift) > loud)
             const bool first = !(seen >> j & 1), any = top > -INFINITY;
             const float up = first ? (any ? top - lift : 0.0f) : fmaxf(top, before) - lift;                 // (t has the lift in it)
             const float down = first ? 1.0f : __builtin_amdgcn_exp2f(-up);                    // (a first maximum: there are no sums yet)
+            mine[16 * j] = lift;                // (each lane reads back what it wrote)
             seen |= (uint32_t)any << j;
             m[j] += up;
             l[j] *= down;
+            if (end[j] != 0) highest = fmaxf(highest, lift);
+            lowest = fminf(lowest, lift);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -311,6 +327,8 @@ struct Rows {
 #pragma unroll
             for (int c = 0; c < 2 * W; ++c) acc[j][c] *= down;
         }
+        low = -__int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(max_over_64_lanes(-lowest))));      // (scalars)
+        reach = __uint_as_float((uint32_t)(kTop + 127 - (int)__int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(max_over_64_lanes(highest))))) << 23);
         unseen = seen == (1u << NT) - 1 ? kNone : INFINITY;
     }
     // A tile's weights of 32 keys from their scores above m: their sum, and with the values' steps the operand of the second product.  Tokens 0, 2 and 1, 3 of a group of four lie
@@ -402,7 +420,7 @@ struct Rows {
                     over = fmaxf(over, t[j][h][i]);
                 }
             }
-        raise(t, over, tops);
+        raise(t, vs, over, tops);
         Operand p[NT];
 #pragma unroll
         for (int j = 0; j < NT; ++j) weigh<EDGE>(j, t[j], vs, p[j]);

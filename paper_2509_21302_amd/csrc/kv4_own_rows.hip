@@ -41,7 +41,7 @@ __global__ __launch_bounds__(256, (NT == 1 || (D == 64 && NT == 2) ? 3 : 2)) voi
 {
     constexpr int C = D / 16, kPad = D + 4;
     __shared__ __align__(16) float area[4][16 * kPad];
-    __shared__ float tops[4][16], totals[4][16];
+    __shared__ float tops[4][16], totals[4][16], lifts[4][16 * NT];
     const Kv4Attention &a = w.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
     // Heads first, parts next, then tiles from the last one on, where rows see most, sequences last: blocks that run together have keys in common (those of a head on one of the eight
@@ -72,7 +72,7 @@ __global__ __launch_bounds__(256, (NT == 1 || (D == 64 && NT == 2) ? 3 : 2)) voi
         r.take_queries(j, mine, lane);
         lanes_exchange_fence();
     }
-    r.start(r.highest_exponent());
+    r.start(r.highest_exponent(), lifts[wave]);
     Keys<D, 1, false> keys;
     if (t0 < stop) keys.begin(a, b, head, last, t0, 32, lane);
     r.run(keys, t0, 32, full, last, stop, g);

@@ -82,7 +82,7 @@ __global__ __launch_bounds__(256, (NT == 1 ? 3 : 2)) void kv4_shared_rows_kernel
 {
     constexpr int C = D / 16, kPad = D + 4;
     __shared__ __align__(16) float area[4][16 * kPad];
-    __shared__ float tops[4][16], totals[4][16];
+    __shared__ float tops[4][16], totals[4][16], lifts[4][16 * NT];
     __shared__ Map::Place places[4];
     const Kv4Attention &a = w.a;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tiles = NT == 1 ? 1 : w.tiles, heads = a.pages.heads * tiles;
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(256, (NT == 1 ? 3 : 2)) void kv4_shared_rows_kernel
             r.end[j] = row < rows ? visible(a, seq, row / w.group) : 0;
             r.take_queries(j, area[j], lane);
         }
-        r.start(r.highest_exponent());
+        r.start(r.highest_exponent(), lifts[wave]);
         r.run(keys, t0, 128, full, last, end, g);
         __syncthreads();                        // the area had the queries
 #pragma unroll

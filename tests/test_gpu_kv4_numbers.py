@@ -163,6 +163,15 @@ def test_results_are_not_too_small(d, heads, kv_heads, q_lens, kv_lens):
     assert abs((got @ want) / (want @ want) - 1) <= 5e-5
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("power", [20, 40, 110])
+@pytest.mark.parametrize("name", KERNELS)
+def test_values_of_another_size_where_rows_do_not_see_them(name, power):
+    """Two values near the end whose steps are 2^power of the others': rows in front of them are as exact as ever (weights of neighbouring rows are scaled each by its own)."""
+    p, sizes = problem(name, v_scale=at_the_end(KERNELS[name][5], (1, 3), 2.0 ** power))
+    check(p, sizes)
+
+
 def sharp_bound(turned, keys, values, scale):
     """(the result of one row, how far off each of its channels may be); turned and keys in the turned basis, where products are taken.  A channel of the query is an fp16 number, off by 2^-11
     of itself at most, so score j is off by D_j = 2^-11 times the sum of the magnitudes of its product's terms.  With o the result, weights times e^+-D_j change it by
