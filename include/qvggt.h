@@ -508,12 +508,12 @@ int qvggt_calib_descent_step(float *theta, const float *grad, int n, float lr, f
  *   j over the keys 0 .. len - n + i with causal = 1 (the queries are the sequence's last n tokens), 0 .. len - 1 with causal = 0.  A query that sees no key gives zeros,
  *   one that is no number (an infinity or a NaN in its head) NaN.
  *   Q: bf16 or f32 [T, q_heads, d], token t at q_stride * t elements.  q_heads a multiple of kv_heads.  signs as given to qvggt_kv4_append.  q_starts: int32 [seqs + 1], not falling;
- *   kv_lens: int32 [seqs]; page_table: int32 [seqs, table_width].  max_q and max_kv: at least every n and len (they decide how the work is cut up; of a longer
- *   sequence the first max_q queries are answered, each from those of the first max_kv keys that it would see),
- *   max_kv <= table_width * page_tokens.  What lies in pages behind a sequence's end, and entries of page_table behind its last page, may be anything.  An entry in use that is no page of
+ *   kv_lens: int32 [seqs]; page_table: int32 [seqs, table_width].  max_q and max_kv: at least every n and len (they decide how the work is cut up; of a longer sequence the first max_q
+ *   queries are answered, each from those of the first max_kv keys that it would see), max_kv <= table_width * page_tokens.  What lies in pages behind a sequence's end, and entries of page_table behind its last page, may be anything.  An entry in use that is no page of
  *   the pool gives wrong results for its sequence, and nothing is read outside the pool.  seqs <= 65535.  out: bf16 [T, q_heads, d]; rows of no sequence are not written.
- *   workspace: qvggt_kv4_attention_workspace_bytes of the same sizes, 16-byte aligned, NULL where that is 0.  Scores, weights and sums are fp32, queries and weights are rounded to fp16
- *   (11 bits) for the products.  Sums in a fixed order: the same call gives the same bits.
+ *   workspace: qvggt_kv4_attention_workspace_bytes of the same sizes, 16-byte aligned, NULL where that is 0.  Scores, weights and sums are fp32, queries (float32 ones too) and weights
+ *   times the values' steps are rounded to the nearest fp16 (11 bits) for the products; those weights reach down to 2^-31 of the largest at the largest step that the row sees.  Sums in a
+ *   fixed order: the same call gives the same bits.
  * T * heads at most 2^27 in qvggt_kv4_append and qvggt_kv4_read; in qvggt_kv4_attention max_kv at most 2^30 and seqs * kv_heads * ceil(max_q * (q_heads / kv_heads) / 64) at most 2^23.
  * QVGGT_ERR_SHAPE for sizes outside these limits, QVGGT_ERR_ARG for a scale that is not finite or a causal other than 0 and 1.  int32 arrays and tables need 16-byte aligned pointers as
  * everything else.

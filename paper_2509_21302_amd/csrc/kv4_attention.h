@@ -7,7 +7,7 @@
 // The codes go to the matrix cores as fp16 numbers without a conversion: u = code + 8 in the low four bits of a half word is the subnormal u 2^-24, one nibble
 // up it is 16 u 2^-24, both exact (the instruction does not flush them), so a word of 8 codes is four operands after one shift and four ands.  The 16 of the odd channels is taken
 // out of the queries in the one product and out of the sum in the other, and the 8 that every code is too large by comes off in the accumulator that the first product starts from
-// and, in the second, with the sum of the weights that one more instruction on eights makes.  Queries are fp16 with a power of two common to a wave, weights fp16 scaled so
+// and, in the second, every few hundred steps with the sum of the weights that one more instruction on eights makes.  Queries are fp16 with a power of two common to a wave, weights fp16 scaled so
 // that they reach down to 2^-31 of the largest: 11 bits, against 8 of a bf16 that the result is rounded to.
 //
 // A wave takes 32 tokens a step: scores of 32 tokens x 16 rows (keys x queries), exp2, weights, sums (values x weights) -- the accumulators of the first product have, lane by lane, the
@@ -118,7 +118,7 @@ struct Keys {
             part[h] = head_base + (size_t)min(max(page[h], 0), num_pages - 1) * page_bytes;
         }
     }
-    // ONCE: nobody else reads these bytes, and the caches need not keep them
+    // ONCE: the caches need not keep these bytes, which nobody else reads (or one block more, where a head has two tiles of rows in shared blocks: it reads memory again)
     template <int N>
     __device__ static void words(const uint8_t *base, uint32_t offset, uint32_t (&w)[N])
     {

@@ -74,9 +74,9 @@ struct Quad {
     }
 };
 
-// Keys and values of a quad's tokens.  16411 tokens of 8 heads x 128 channels in f32, 152 MB: 44 us, 3.5 TB/s; bound by ~600 vector instructions a wave and, half of its time, by the chain
-// slots, positions, angles and rows.  Few tokens: that chain alone (one token 3.5 us with its launch).  The values' rows are read past the caches (47 us within them); the keys' are not: a
-// channel and its partner read the same row.
+// Keys and values of a quad's tokens.  16411 tokens of 8 heads x 128 channels in f32, 152 MB: 40 us, 3.8 TB/s; bound by ~600 vector instructions a wave (0.74 of the cycles issue one) and by the chain
+// slots, positions, angles and rows.  Few tokens: that chain alone (one token 3.5 us with its launch).  The values' rows are read past the caches (47 us for 44 within them); the keys' are not:
+// a channel and its partner read the same row.
 template <int D, bool f32>
 __global__ __launch_bounds__(256) void kv4_append_kernel(const void *K, const void *V, int T, long long k_stride, long long v_stride, Rope rope, const int8_t *signs,
                                                          const int32_t *slots, Kv4Pages pages)
@@ -137,7 +137,8 @@ __device__ inline void store_channels(void *row, bool f32, int first, const floa
     }
 }
 
-// What a quad's tokens hold: codes times step, turned back.  Bound by memory: the same 16411 tokens into bf16, 84 MB, 23 us, 3.7 TB/s; the rows leave past the caches (24 us through them).
+// What a quad's tokens hold: codes times step, turned back.  The same 16411 tokens into bf16, 84 MB: 22 us, 3.8 TB/s, with a vector instruction issuing in 0.78 of the cycles; the rows leave past the
+// caches (24 us for 23 through them).
 template <int D>
 __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Pages pages, const int32_t *slots, int T, const int8_t *signs, bool f32, void *K, void *V)
 {

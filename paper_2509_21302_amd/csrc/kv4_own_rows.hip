@@ -2,9 +2,9 @@
 // keys that they see; the four waves of a block go through the same pages at about the same time.
 //
 // What bounds it is the issue of vector and matrix instructions, of which the SIMD overlaps little: taking 4-bit words apart and exp2 on the one side, two products on the other (a prompt of
-// 12289 tokens, 32 heads on 8, 128 channels: 0.81 of the cycles have a vector or matrix instruction issuing, the matrix cores are busy in 0.41; 1.27 ms, 0.97 PFLOP/s of what rows see.
-// 1374 queries on 68700 keys, 16 heads x 64: 0.60 ms, 0.64 PFLOP/s).  Turning tiles of codes into fp16 numbers in LDS once a block, so that the waves share that work, is no faster
-// (64 keys at a time, or 32, one tile ahead: 1.30 to 1.58 ms): reading them back costs what it saves.
+// 12289 tokens, 32 heads on 8, 128 channels: 0.82 of the cycles have a vector or matrix instruction issuing, the matrix cores are busy in 0.40; 1.32 ms, 0.94 PFLOP/s of what rows see), and, where
+// a wave has four tiles, what two waves a SIMD with one step ahead wait for (1374 queries on 68700 keys, 16 heads x 64: 0.64 and 0.28 of the cycles; 0.62 ms, 0.62 PFLOP/s).  Turning tiles of codes
+// into fp16 numbers in LDS once a block, so that the waves share that work, is no faster (64 keys at a time, or 32, one tile ahead: 1.30 to 1.58 ms where this was 1.27): reading them back costs what it saves.
 #include "kv4_attention.h"
 #include "kv4_plan.h"
 
@@ -22,7 +22,7 @@ __device__ inline size_t partial_row(const Tiled &w, int b, int head, int row, i
 }
 
 // The sequence with the place'th most keys, of every 64 of them: whichever order a batch has, the longest blocks begin first (448 queries on 1500 keys of 12 sequences at most, 20 heads x 64:
-// 57.7 us in reversed and in random order, 69.3 and 72.1 without).  Not where a wave has four tiles, whose registers are full (a frame over 50: 633 us for 612) and whose blocks are many
+// 57.7 us in reversed and in random order, 69.3 and 72.1 without; 55 as it is now).  Not where a wave has four tiles, whose registers are full (a frame over 50: 633 us for 612) and whose blocks are many
 // or of one sequence.
 __device__ inline int longest(const Kv4Attention &a, int place, int lane)
 {

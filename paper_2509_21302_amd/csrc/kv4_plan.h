@@ -26,8 +26,8 @@ inline Kv4Shares kv4_shares(int seqs, int max_q, int max_kv, int q_heads, int kv
     const long long segments = (long long)seqs * kv_heads * p.tiles;
     while (segments * (kv4_div_up(max_kv, 1LL << p.unit_shift) + 4) >= 1LL << 30) ++p.unit_shift;
     const long long units = segments * kv4_div_up(max_kv, 1LL << p.unit_shift);
-    // Whole heads: where even the longest is not worth a join, where the blocks are many enough to even out by themselves, and where every block would go through more lengths than
-    // it has keys' worth of time for
+    // Whole heads: where even the longest is not worth a join, where the blocks are many enough to even out by themselves as long as lengths are alike, and where every block would go through
+    // more lengths than it has keys' worth of time for
     if (max_kv <= 1024 || segments >= 4 * resident || seqs > 512) return p;
     const long long blocks = kv4_div_up(units, p.least);
     p.blocks = (int)(blocks < resident ? blocks : resident);

@@ -1,10 +1,11 @@
 // Attention over the 4-bit key/value cache for up to 64 rows a key head (single tokens, a few tokens): the waves of a block share the rows and take steps of 32 keys in turn.
-// What bounds it is the way of the pages out of memory: one sequence of a megatoken, 8 heads x 128, 190 us, 5.85 TB/s (16 x 64: 214 us, 5.34); 64 sequences to 8192 keys, 287 MB, 60 us and
+// What bounds it is the way of the pages out of memory: one sequence of a megatoken, 8 heads x 128, 189 us, 5.86 TB/s (16 x 64: 217 us, 5.25); 64 sequences to 8192 keys, 287 MB, 60 us and
 // 5 for the join.  About 10 us of a call are the way lengths, page table, pages at its start and that join.
 //
 // The keys of all sequences and heads, in units of a block's step, are laid end to end and cut into as many even shares as the chip holds blocks at a time: lengths of a batch may
-// differ as they like.  A block goes through its share sequence by sequence and head by head; where a head's keys are cut, its blocks leave partial sums, at most two each, and the join
-// puts them together.  Where there are few keys, or many more heads than blocks at a time, every head has a block of its own and nothing is joined.
+// differ as they like, up to 512 sequences and four heads for every block that the chip holds.  A block goes through its share sequence by sequence and head by head; where a head's keys are cut, its blocks leave partial sums, at most two each, and the join
+// puts them together.  Where there are few keys, or more sequences or heads than that, every head has a block of its own and nothing is joined: one sequence far longer
+// than the others is what such a call waits for.
 #include "kv4_attention.h"
 #include "kv4_plan.h"
 
