@@ -61,6 +61,7 @@ typedef enum {
 } qvggt_status;
 
 typedef enum { QVGGT_BF16 = 0, QVGGT_F32 = 1 } qvggt_dtype;
+typedef enum { QVGGT_NORM_NONE = 0, QVGGT_NORM_LAYER = 1, QVGGT_NORM_RMS = 2 } qvggt_norm;
 
 /* Human-readable name of a status code (host pointer to a static string). */
 const char *qvggt_status_string(int status);
@@ -529,6 +530,49 @@ int qvggt_kv4_attention(const void *Q, int q_dtype, int T, long long q_stride, i
                         const int32_t *positions, const int8_t *signs, float scale, int causal, const void *cache, int num_pages, int page_tokens, int kv_heads, int d,
                         const int32_t *page_table, int table_width, const int32_t *q_starts, const int32_t *kv_lens, int seqs, int max_q, int max_kv, void *out,
                         void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * What stands between and around the layers of a block that keeps no cache: heads of queries and keys normalised and rotated, attention of whole sequences, the residual stream with its norms.
+ * A norm (QVGGT_NORM_*) of n channels is (x - mean) / sqrt(variance + eps), x / sqrt(mean of squares + eps), or x as it is; then times a gain and plus a bias (f32 [n], NULL: without;
+ * with QVGGT_NORM_NONE too).  eps >= 0.  Arithmetic, sums and statistics are fp32, results are rounded once, to the nearest.  An infinity or a NaN stays in its own row (head), and in the rows
+ * of attention that see it.
+ *
+ * qvggt_heads_norm_rope:  every head of T tokens' queries and keys (d = 64 or 128 channels): norm, then the rotation of qvggt_kv4_append by positions with several axes: the angle number p
+ *   of a token is the one at column p of row positions[axis][token] of the table, axis = pair_axis[p], or p * axes / (rope_dim / 2) where pair_axis is NULL (sections of equal length, one
+ *   behind the other).  positions: int32 [axes, T], 1 <= axes <= 4 (rows outside the table are taken as its first or last); pair_axis: uint8 [rope_dim / 2] (numbers past the last axis are taken
+ *   as it).  rope, rope_dim and rope_pair as there; rope = NULL: no rotation.  Q, K, Q_out, K_out: all bf16 or all f32, token t at its stride * t elements, heads one after another (strides a
+ *   multiple of 16 bytes, of outputs no less than a row).  An output may be its own input; otherwise outputs overlap neither inputs nor each other.  q_heads or kv_heads = 0: without queries, or
+ *   keys.  T * (q_heads + kv_heads) at most 2^27.
+ *
+ * qvggt_attention:  for every sequence b, its n = q_starts[b + 1] - q_starts[b] query tokens (rows q_starts[b] .. of Q) over its len keys and values, rows kv_starts[b] .. of K and V:
+ *     out[i, h, :] = sum_j softmax_j( scale * <q[i, h], k[j, h']> ) v[j, h'],     h' = h / (q_heads / kv_heads),
+ *   j over the keys 0 .. len - n + i with causal = 1 (the queries are the sequence's last n tokens), 0 .. len - 1 with causal = 0.  A query that sees no key gives zeros.
+ *   dtype: QVGGT_BF16, of Q, K, V and out.  Q [T, q_heads, d], K and V [S, kv_heads, d] at their strides (elements, multiples of 8; k_stride and v_stride below 2^24); d = 64 or 128; q_heads a
+ *   multiple of kv_heads.  q_starts: int32 [seqs + 1], not falling.  kv_lens = NULL: kv_starts is int32 [seqs + 1] and len the difference (whole prompts: kv_starts = q_starts); otherwise
+ *   kv_starts and kv_lens are int32 [seqs] (a buffer for every sequence that its tokens are added to, for example).  Starts and lengths are read on the device: a call can be captured and replayed
+ *   with others.  Those that lead outside of T and S are cut.  max_q and max_kv: at least every n and len (they decide how the work is cut up; of a longer sequence the first max_q queries are
+ *   answered, each from those of the first max_kv keys that it would see).  Rows of K and V that no sequence names, or that no query sees, may be anything.  seqs <= 65535.
+ *   out: bf16 [T, q_heads, d]; rows of no sequence are not written.  It overlaps no input.  workspace: qvggt_attention_workspace_bytes of the same sizes, 16-byte aligned, NULL where that is 0;
+ *   two calls that may run at the same time take one each.  Scores, maxima and sums are fp32, weights are rounded to the nearest bf16 (8 bits), in the sum that they are divided by as well.  Sums in
+ *   a fixed order: the same call gives the same bits.  max_kv at most 2^30, seqs * kv_heads * ceil(max_q * (q_heads / kv_heads) / 32) at most 2^23.  int32 arrays need 4-byte alignment only.
+ *
+ * qvggt_residual_norm:  of M tokens of C channels (a multiple of 8 from 8 to 8192), y a block's output, x the residual stream:
+ *     x'[t] = x[t] + scale * gate[r] * norm_post(y[t]),       h[t] = norm(x'[t]) * (1 + mod_scale[r]) + mod_shift[r]
+ *   post_norm, post_gain, post_bias and norm, gain, bias: the two norms.  scale: f32 [C].  gate, mod_scale, mod_shift: bf16 or f32 [cond_rows, C], row r at cond_stride * r elements (parts of the
+ *   rows of one product, for example; a multiple of 16 bytes); r = row_of[t] (int32 [M]; rows outside are taken as the first or last), or without row_of 0 where cond_rows = 1, t where cond_rows = M
+ *   (QVGGT_ERR_SHAPE for others).  scale, gate, mod_scale, mod_shift may be NULL: left out.  y = NULL: x' = x.  Outputs: x_out, of x's type, h, bf16 or f32; either may be NULL.  h is of x'
+ *   before it is rounded.  x_out may be x, and h may be x or y where it has the same type (QVGGT_ERR_ARG for other types, and for x_out = h or x_out = y); otherwise outputs overlap nothing.
+ */
+int qvggt_heads_norm_rope(const void *Q, const void *K, int dtype, int T, long long q_stride, long long k_stride, int q_heads, int kv_heads, int d, int norm, float eps, const float *q_gain,
+                          const float *q_bias, const float *k_gain, const float *k_bias, const float *rope, int rope_rows, int rope_dim, int rope_pair, const int32_t *positions, int axes,
+                          const uint8_t *pair_axis, void *Q_out, void *K_out, long long q_out_stride, long long k_out_stride, void *stream);
+size_t qvggt_attention_workspace_bytes(int T, int seqs, int max_q, int max_kv, int q_heads, int kv_heads, int d);
+int qvggt_attention(const void *Q, const void *K, const void *V, int dtype, int T, int S, long long q_stride, long long k_stride, long long v_stride, int q_heads, int kv_heads, int d,
+                    float scale, int causal, const int32_t *q_starts, const int32_t *kv_starts, const int32_t *kv_lens, int seqs, int max_q, int max_kv, void *out, void *workspace,
+                    size_t workspace_bytes, void *stream);
+int qvggt_residual_norm(const void *x, int x_dtype, const void *y, int y_dtype, int M, int C, int post_norm, const float *post_gain, const float *post_bias, const float *scale,
+                        const void *gate, int norm, const float *gain, const float *bias, const void *mod_scale, const void *mod_shift, int cond_dtype, int cond_rows, long long cond_stride,
+                        const int32_t *row_of, float eps, void *x_out, void *h, int h_dtype, void *stream);
 
 /*
  * Measurement helper (used by the benchmark, not by the path): a register-only loop of the matrix instruction that the GEMMs of

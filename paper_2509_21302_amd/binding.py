@@ -46,12 +46,17 @@ EXPORTS = [
     "qvggt_linear_e2m3_any", "qvggt_layer_workspace_bytes", "qvggt_layer_statistics", "qvggt_layer_codes",
     "qvggt_rotate_rows", "qvggt_calib_workspace_bytes", "qvggt_calib_loss_grad", "qvggt_calib_descent_step",
     "qvggt_kv4_page_bytes", "qvggt_kv4_append", "qvggt_kv4_read", "qvggt_kv4_attention_workspace_bytes", "qvggt_kv4_attention",
+    "qvggt_heads_norm_rope", "qvggt_attention_workspace_bytes", "qvggt_attention", "qvggt_residual_norm",
 ]
 
 
 # the entry points that _call.linear knows, in its order
 LINEAR_KINDS = ("qvggt_linear", "qvggt_linear_e2m3_any", "qvggt_gelu_linear_e2m3", "qvggt_linear_i8", "qvggt_linear_i8b")
 PACKED, E2M3, GELU, INT8, INT8_BLOCKS = range(5)
+
+
+# the norms of qvggt_heads_norm_rope and qvggt_residual_norm, by their numbers
+NORMS = ("none", "layer", "rms")
 
 
 # ... and those that its functions of their own call, in its order
@@ -205,6 +210,14 @@ def load_library() -> C.CDLL:
     lib.qvggt_kv4_read.argtypes = [vp, i, i, i, i, vp, vp, i, i, vp, vp, vp]
     lib.qvggt_kv4_attention_workspace_bytes.restype = sz
     lib.qvggt_kv4_attention_workspace_bytes.argtypes = [i, i, i, i, i, i, i]
+    lib.qvggt_heads_norm_rope.restype = i
+    lib.qvggt_heads_norm_rope.argtypes = [vp, vp, i, i, ll, ll, i, i, i, i, f, vp, vp, vp, vp, vp, i, i, i, vp, i, vp, vp, vp, ll, ll, vp]
+    lib.qvggt_attention_workspace_bytes.restype = sz
+    lib.qvggt_attention_workspace_bytes.argtypes = [i, i, i, i, i, i, i]
+    lib.qvggt_attention.restype = i
+    lib.qvggt_attention.argtypes = [vp, vp, vp, i, i, i, ll, ll, ll, i, i, i, f, i, vp, vp, vp, i, i, i, vp, vp, sz, vp]
+    lib.qvggt_residual_norm.restype = i
+    lib.qvggt_residual_norm.argtypes = [vp, i, vp, i, i, i, i, vp, vp, vp, vp, i, vp, vp, vp, vp, i, i, ll, vp, f, vp, vp, i, vp]
     lib.qvggt_kv4_attention.restype = i
     lib.qvggt_kv4_attention.argtypes = [vp, i, i, ll, i, vp, i, i, i, vp, vp, f, i, vp, i, i, i, i, vp, i, vp, vp, i, i, i, vp, vp, sz, vp]
     lib.qvggt_workspace_bytes.restype = sz
@@ -760,3 +773,106 @@ def qvggt_kv4_attention(Q, signs, scale, causal, cache, page_tokens, kv_heads, p
                                               _whole(page_table, "page_table", torch.int32, seqs * width), width, _whole(q_starts, "q_starts", torch.int32, seqs + 1),
                                               _whole(kv_lens, "kv_lens", torch.int32, seqs), seqs, int(max_q), int(max_kv), _ptr(out), _ptr(workspace),
                                               0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)), "qvggt_kv4_attention")
+
+
+# ---- around a block's layers
+def _norm_code(norm) -> int:
+    if norm not in NORMS:
+        raise ValueError(f"a norm is one of {', '.join(NORMS)}, not {norm!r}")
+    return NORMS.index(norm)
+
+
+def _here(where, *tensors):
+    """These calls run on the current device's current stream: tensors of another device are refused."""
+    at = torch.cuda.current_device() if any(t is not None and t.is_cuda for t in tensors) else None
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != at:
+            raise ValueError(f"{where}: a tensor of another device than the current one")
+
+
+def qvggt_heads_norm_rope(Q, K, Q_out, K_out, norm="none", eps=1e-6, q_gain=None, q_bias=None, k_gain=None, k_bias=None, rope=None, positions=None, rope_pair=0, pair_axis=None,
+                          stream=None):
+    """Q [T, q_heads, d] and K [T, kv_heads, d] (either may be None, with its output) into Q_out and K_out, which may be the same tensors."""
+    some = Q if Q is not None else K
+    T, _, d = some.shape
+    heads, at, strides, outs, out_strides = [], [], [], [], []
+    for x, y, name in ((Q, Q_out, "Q"), (K, K_out, "K")):
+        if x is None:
+            for items in (heads, strides, out_strides):
+                items.append(0)
+            at.append(None)
+            outs.append(None)
+            continue
+        if x.dim() != 3 or x.shape[0] != T or x.shape[2] != d or x.dtype != some.dtype:
+            raise ValueError(f"{name}: [tokens, heads, channels] of the other's tokens, channels and type")
+        if y is None or y.shape != x.shape or y.dtype != x.dtype:
+            raise ValueError(f"{name}_out: the shape and type of {name}")
+        p, stride = _heads_of(x, name)
+        o, out_stride = _heads_of(y, name + "_out")
+        heads.append(x.shape[1])
+        at.append(p)
+        strides.append(stride)
+        outs.append(o)
+        out_strides.append(out_stride)
+    axes = 0
+    if positions is not None and rope is not None:
+        axes = positions.shape[0] if positions.dim() == 2 else 1
+    table, rows, dim, _ = _rope_of(rope, positions, axes * T)
+    gains = [_whole(t, name, torch.float32, d) for t, name in ((q_gain, "q_gain"), (q_bias, "q_bias"), (k_gain, "k_gain"), (k_bias, "k_bias"))]
+    _here("qvggt_heads_norm_rope", Q, K, Q_out, K_out, q_gain, q_bias, k_gain, k_bias, rope, positions, pair_axis)
+    _check(load_library().qvggt_heads_norm_rope(at[0], at[1], _dtype_code(some), T, strides[0], strides[1], heads[0], heads[1], d, _norm_code(norm), float(eps), *gains, table, rows, dim,
+                                                int(rope_pair), None if rope is None else _ptr(positions), axes,
+                                                None if rope is None else _whole(pair_axis, "pair_axis", torch.uint8, dim // 2), outs[0], outs[1], out_strides[0], out_strides[1],
+                                                _stream(stream)), "qvggt_heads_norm_rope")
+
+
+def qvggt_attention_workspace_bytes(T: int, seqs: int, max_q: int, max_kv: int, q_heads: int, kv_heads: int, d: int) -> int:
+    return int(load_library().qvggt_attention_workspace_bytes(int(T), int(seqs), int(max_q), int(max_kv), int(q_heads), int(kv_heads), int(d)))
+
+
+def qvggt_attention(Q, K, V, scale, causal, q_starts, kv_starts, kv_lens, max_q, max_kv, out, workspace, stream=None):
+    """Q [T, q_heads, d], K and V [S, kv_heads, d], out [T, q_heads, d], all bf16; q_starts int32 [seqs + 1]; kv_starts int32 [seqs + 1] with kv_lens None, both [seqs] otherwise."""
+    T, heads, d = Q.shape
+    S, kv_heads, _ = K.shape
+    if V.shape != K.shape or K.shape[2] != d or not Q.dtype == K.dtype == V.dtype:
+        raise ValueError("K and V: one shape, channels and type of Q")
+    at_q, q_stride = _heads_of(Q, "Q")
+    at_k, k_stride = _heads_of(K, "K")
+    at_v, v_stride = _heads_of(V, "V")
+    if out.shape != Q.shape or out.dtype != Q.dtype:
+        raise ValueError("out: the shape and type of Q")
+    seqs = q_starts.numel() - 1
+    if seqs < 0:
+        raise ValueError("q_starts: an end for every sequence")
+    _here("qvggt_attention", Q, K, V, q_starts, kv_starts, kv_lens, out, workspace)
+    _check(load_library().qvggt_attention(at_q, at_k, at_v, _dtype_code(Q), T, S, q_stride, k_stride, v_stride, heads, kv_heads, d, float(scale), int(causal),
+                                          _whole(q_starts, "q_starts", torch.int32, seqs + 1), _whole(kv_starts, "kv_starts", torch.int32, seqs + (kv_lens is None)),
+                                          _whole(kv_lens, "kv_lens", torch.int32, seqs), seqs, int(max_q), int(max_kv), _ptr(out), _ptr(workspace),
+                                          0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)), "qvggt_attention")
+
+
+def qvggt_residual_norm(x, y, x_out, h, post_norm="none", post_gain=None, post_bias=None, scale=None, gate=None, norm="none", gain=None, bias=None, mod_scale=None, mod_shift=None,
+                        row_of=None, eps=1e-6, stream=None):
+    """x and y [M, C] (y may be None), x_out of x's type and h [M, C] (either may be None); gate, mod_scale and mod_shift [rows, C], of one type and with one distance between rows."""
+    M, C = x.shape
+    for t, name in ((y, "y"), (x_out, "x_out"), (h, "h")):
+        if t is not None and t.shape != x.shape:
+            raise ValueError(f"{name}: the shape of x")
+    if x_out is not None and x_out.dtype != x.dtype:
+        raise ValueError("x_out: the type of x")
+    cond = [t for t in (gate, mod_scale, mod_shift) if t is not None]
+    rows = stride = dtype = 0
+    if cond:
+        rows, dtype = cond[0].shape[0], _dtype_code(cond[0])
+        stride = cond[0].stride(0) if rows > 1 else C
+        for t in cond:
+            if not t.is_cuda:
+                raise ValueError("qvggt takes device tensors only")
+            if t.dim() != 2 or t.shape != (rows, C) or t.dtype != cond[0].dtype or t.stride(1) != 1 or rows > 1 and t.stride(0) != stride:
+                raise ValueError("gate, mod_scale, mod_shift: [rows, C] of one type, one number of rows and one distance between them")
+    parts = [None if t is None else t.data_ptr() for t in (gate, mod_scale, mod_shift)]
+    vectors = [_whole(t, name, torch.float32, C) for t, name in ((post_gain, "post_gain"), (post_bias, "post_bias"), (scale, "scale"), (gain, "gain"), (bias, "bias"))]
+    _here("qvggt_residual_norm", x, y, x_out, h, post_gain, post_bias, scale, gate, gain, bias, mod_scale, mod_shift, row_of)
+    _check(load_library().qvggt_residual_norm(_ptr(x), _dtype_code(x), _ptr(y), 0 if y is None else _dtype_code(y), M, C, _norm_code(post_norm), vectors[0], vectors[1], vectors[2],
+                                              parts[0], _norm_code(norm), vectors[3], vectors[4], parts[1], parts[2], dtype, rows, stride, _whole(row_of, "row_of", torch.int32, M),
+                                              float(eps), _ptr(x_out), _ptr(h), 0 if h is None else _dtype_code(h), _stream(stream)), "qvggt_residual_norm")

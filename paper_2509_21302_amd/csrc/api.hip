@@ -1,6 +1,9 @@
 // C ABI of the qvggt library: argument validation on the host, then kernel launches on the
 // caller's stream.  Declarations and the meaning of every argument are in include/qvggt.h.
 #include "qvggt_common.h"
+#include "attention.h"
+#include "attention_plan.h"
+#include "block_rows.h"
 #include "kv4.h"
 #include "kv4_plan.h"
 #include "../../include/qvggt.h"
@@ -928,6 +931,88 @@ int qvggt_kv4_attention(const void *Q, int q_dtype, int T, long long q_stride, i
                                 pages_of(cache, num_pages, page_tokens, kv_heads), page_table, table_width, q_starts, kv_lens, seqs, max_q, max_kv,
                                 static_cast<uint16_t *>(out), workspace};
     return hip_status(qvggt::run_kv4_attention(a, d, static_cast<hipStream_t>(stream)));
+}
+
+// ---- around a block's layers
+namespace {
+bool valid_norm(int norm) { return norm == QVGGT_NORM_NONE || norm == QVGGT_NORM_LAYER || norm == QVGGT_NORM_RMS; }
+bool valid_eps(float eps) { return std::isfinite(eps) && eps >= 0.0f; }
+constexpr long long kMostStride = 1 << 24;      // elements from a key to the next one: 64 of them are an offset of 32 bits
+bool valid_packed(int T, int S, int seqs, int max_q, int max_kv, int q_heads, int kv_heads, int d)
+{
+    return T >= 0 && S >= 0 && seqs >= 0 && seqs <= 65535 && max_q >= 0 && max_kv >= 0 && max_kv <= (1 << 30) && (d == 64 || d == 128) && kv_heads >= 1 && kv_heads <= 65535 &&
+           q_heads >= kv_heads && q_heads <= 65535 && q_heads % kv_heads == 0 && (long long)max_q * (q_heads / kv_heads) <= (1 << 30) &&
+           (long long)seqs * kv_heads * qvggt::attention_div_up((long long)max_q * (q_heads / kv_heads), qvggt::kAttentionTile) <= qvggt::kAttentionMostBlocks;
+}
+}  // namespace
+
+int qvggt_heads_norm_rope(const void *Q, const void *K, int dtype, int T, long long q_stride, long long k_stride, int q_heads, int kv_heads, int d, int norm, float eps, const float *q_gain,
+                          const float *q_bias, const float *k_gain, const float *k_bias, const float *rope, int rope_rows, int rope_dim, int rope_pair, const int32_t *positions, int axes,
+                          const uint8_t *pair_axis, void *Q_out, void *K_out, long long q_out_stride, long long k_out_stride, void *stream)
+{
+    if (!valid_dtype(dtype)) return QVGGT_ERR_DTYPE;
+    const long long q_row = (long long)q_heads * d, k_row = (long long)kv_heads * d;
+    if (T < 0 || !qvggt::kv4_valid_head(d) || q_heads < 0 || kv_heads < 0 || q_heads > 65535 || kv_heads > 65535 || (long long)T * (q_heads + kv_heads) > 1 << 27 || q_stride < 0 ||
+        k_stride < 0 || !valid_rope(rope, rope_rows, rope_dim, rope_pair, d) || (rope && (axes < 1 || axes > 4)) ||
+        (T > 1 && ((q_heads > 0 && q_out_stride < q_row) || (kv_heads > 0 && k_out_stride < k_row))))
+        return QVGGT_ERR_SHAPE;
+    if (!valid_norm(norm) || !valid_eps(eps)) return QVGGT_ERR_ARG;
+    if (T == 0 || q_heads + kv_heads == 0) return QVGGT_OK;
+    if ((q_heads > 0 && (!Q || !Q_out)) || (kv_heads > 0 && (!K || !K_out)) || (rope && !positions)) return QVGGT_ERR_NULL;
+    const int vector = dtype == QVGGT_F32 ? 4 : 8;            // elements of 16 bytes
+    if (!aligned16(Q) || !aligned16(K) || !aligned16(Q_out) || !aligned16(K_out) || q_stride % vector != 0 || k_stride % vector != 0 || q_out_stride % vector != 0 ||
+        k_out_stride % vector != 0 || !aligned16(q_gain) || !aligned16(q_bias) || !aligned16(k_gain) || !aligned16(k_bias) || !aligned16(rope) || !aligned16(positions) ||
+        !aligned16(pair_axis))
+        return QVGGT_ERR_ALIGN;
+    const qvggt::HeadsNormRope a{{Q, K}, {Q_out, K_out}, {q_stride, k_stride}, {q_out_stride, k_out_stride}, {q_heads, kv_heads}, {q_gain, k_gain}, {q_bias, k_bias}, T, dtype == QVGGT_F32,
+                                 norm, eps, rope, rope_rows, rope_dim, rope_pair, axes, positions, pair_axis};
+    return hip_status(qvggt::run_heads_norm_rope(a, d, static_cast<hipStream_t>(stream)));
+}
+
+size_t qvggt_attention_workspace_bytes(int T, int seqs, int max_q, int max_kv, int q_heads, int kv_heads, int d)
+{
+    return valid_packed(T, 0, seqs, max_q, max_kv, q_heads, kv_heads, d) ? qvggt::attention_plan(seqs, max_q, max_kv, q_heads, kv_heads, d).bytes : 0;
+}
+
+int qvggt_attention(const void *Q, const void *K, const void *V, int dtype, int T, int S, long long q_stride, long long k_stride, long long v_stride, int q_heads, int kv_heads, int d,
+                    float scale, int causal, const int32_t *q_starts, const int32_t *kv_starts, const int32_t *kv_lens, int seqs, int max_q, int max_kv, void *out, void *workspace,
+                    size_t workspace_bytes, void *stream)
+{
+    if (dtype != QVGGT_BF16) return QVGGT_ERR_DTYPE;
+    if (!valid_packed(T, S, seqs, max_q, max_kv, q_heads, kv_heads, d) || q_stride < 0 || k_stride < 0 || v_stride < 0 || k_stride >= kMostStride || v_stride >= kMostStride ||
+        (max_kv > 0 && S == 0))
+        return QVGGT_ERR_SHAPE;
+    if (!std::isfinite(scale) || (causal != 0 && causal != 1)) return QVGGT_ERR_ARG;
+    if (T == 0 || seqs == 0 || max_q == 0) return QVGGT_OK;
+    const size_t need = qvggt::attention_plan(seqs, max_q, max_kv, q_heads, kv_heads, d).bytes;
+    if (!Q || !q_starts || !kv_starts || !out || (max_kv > 0 && (!K || !V)) || (need > 0 && !workspace)) return QVGGT_ERR_NULL;
+    if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || q_stride % 8 != 0 || k_stride % 8 != 0 || v_stride % 8 != 0 || !aligned4(q_starts) || !aligned4(kv_starts) ||
+        !aligned4(kv_lens) || !aligned16(out) || !aligned16(workspace))
+        return QVGGT_ERR_ALIGN;
+    if (workspace_bytes < need) return QVGGT_ERR_WORKSPACE;
+    const qvggt::Attention a{static_cast<const uint16_t *>(Q), static_cast<const uint16_t *>(K), static_cast<const uint16_t *>(V), q_stride, k_stride, v_stride, T, S, q_heads, kv_heads, scale,
+                             causal, q_starts, kv_starts, kv_lens, seqs, max_q, max_kv, static_cast<uint16_t *>(out), workspace};
+    return hip_status(qvggt::run_attention(a, d, static_cast<hipStream_t>(stream)));
+}
+
+int qvggt_residual_norm(const void *x, int x_dtype, const void *y, int y_dtype, int M, int C, int post_norm, const float *post_gain, const float *post_bias, const float *scale,
+                        const void *gate, int norm, const float *gain, const float *bias, const void *mod_scale, const void *mod_shift, int cond_dtype, int cond_rows, long long cond_stride,
+                        const int32_t *row_of, float eps, void *x_out, void *h, int h_dtype, void *stream)
+{
+    const bool conditioned = gate || mod_scale || mod_shift;
+    if (!valid_dtype(x_dtype) || !valid_dtype(y_dtype) || !valid_dtype(h_dtype) || (conditioned && !valid_dtype(cond_dtype))) return QVGGT_ERR_DTYPE;
+    if (M < 0 || C < 8 || C > 8192 || C % 8 != 0 || (conditioned && (cond_rows < 1 || cond_stride < 0 || (!row_of && cond_rows != 1 && cond_rows != M)))) return QVGGT_ERR_SHAPE;
+    // rows are read and written in one pass: an output may be an input of its own type, and no other one
+    if (!valid_norm(post_norm) || !valid_norm(norm) || !valid_eps(eps) || (x_out && (x_out == h || x_out == y)) || (h && ((h == x && h_dtype != x_dtype) || (h == y && h_dtype != y_dtype))))
+        return QVGGT_ERR_ARG;
+    if (M == 0 || (!x_out && !h)) return QVGGT_OK;
+    if (!x) return QVGGT_ERR_NULL;
+    if (!aligned16(x) || !aligned16(y) || !aligned16(post_gain) || !aligned16(post_bias) || !aligned16(scale) || !aligned16(gate) || !aligned16(gain) || !aligned16(bias) ||
+        !aligned16(mod_scale) || !aligned16(mod_shift) || !aligned4(row_of) || !aligned16(x_out) || !aligned16(h) || (conditioned && cond_stride % (cond_dtype == QVGGT_F32 ? 4 : 8) != 0))
+        return QVGGT_ERR_ALIGN;
+    const qvggt::ResidualNorm a{x, y, x_dtype == QVGGT_F32, y_dtype == QVGGT_F32, M, C, post_norm, post_gain, post_bias, scale, gate, norm, gain, bias, mod_scale, mod_shift,
+                                cond_dtype == QVGGT_F32, cond_rows, cond_stride, row_of, eps, x_out, h, h_dtype == QVGGT_F32};
+    return hip_status(qvggt::run_residual_norm(a, static_cast<hipStream_t>(stream)));
 }
 
 // ---- calibration-set arithmetic (Sec. 3.3)

@@ -1,0 +1,475 @@
+// Attention of packed sequences over bf16 keys and values:   out[i, h] = sum_j softmax_j(scale <q[i, h], k[j, h']>) v[j, h'].
+//
+// Rows are the query tokens of a sequence times the query heads that share a key head; a wave has a tile of 32.  Scores are keys x queries and results channels x queries (both
+// v_mfma_f32_32x32x16_bf16): a lane's accumulators are 16 keys of one row, which is what its part of the second product's right operand is made of, if the 16 keys of a step come in the order
+//     element j of lane l  =  key 8 (j / 4) + 4 (l / 32) + j % 4
+// in both operands.  So nothing moves between lanes but a maximum and a sum for every row, and a row's factor is a lane's.  The values' operand has that order from LDS reads that
+// transpose: four keys of sixteen channels a group of sixteen lanes.
+//
+// Keys and values go straight from memory into LDS, 16 bytes a lane, rows as they are.  A row's 16-byte pieces change places by its number (the source address does that), so that reads
+// of 32 rows of keys, and of four rows of values, touch every bank as often as any other.
+//
+// The running maximum of a row is raised when one of its scores exceeds it by more than 2^8 in weight: weights are at most 2^8 then, and sums are multiplied by a factor in few steps.  Weights
+// are rounded to bf16 (to nearest), for the product and for the sum that it is divided by alike.  A row starts from a maximum of -3e38, so that rows that see nothing end with a sum of 0.
+#include "attention.h"
+#include "attention_plan.h"
+#include "lds_transfer.h"
+
+namespace qvggt {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef float float16v __attribute__((ext_vector_type(16)));
+union Operand {
+    uint4 u;
+    uint32_t w[4];
+    short4v s[2];
+    bf16x8 b;
+};
+
+constexpr float kNone = -3.0e38f, kLog2e = 1.4426950408889634f;
+constexpr float kSlack = 8.0f;
+
+struct Cut {
+    Attention a;
+    int group, chunk, splits, tiles;        // query heads of a key head; keys of a part; parts and tiles of rows that there may be
+    float scale2;                           // |scale| log2(e); its sign, and a scale of 0, are in the queries
+    uint32_t flip, keep;                    // ... as masks of pairs of them
+    float *partials;                        // [seqs][key heads][rows][splits][D + 2]: a row's sums, maximum and weights' sum
+};
+
+// ---- a sequence
+struct Sequence {
+    int q0, n, k0;              // first row of the queries, how many are answered, first row of the keys
+    int total, len, limit;      // queries and keys there are, keys that are looked at
+};
+__device__ inline Sequence sequence_of(const Attention &a, int b)
+{
+    Sequence s;
+    s.q0 = min(max(a.q_starts[b], 0), a.T);
+    s.total = min(max(a.q_starts[b + 1], s.q0), a.T) - s.q0;
+    s.n = min(s.total, a.max_q);
+    s.k0 = min(max(a.kv_starts[b], 0), a.S);
+    s.len = min(max(a.kv_lens != nullptr ? a.kv_lens[b] : a.kv_starts[b + 1] - s.k0, 0), a.S - s.k0);
+    s.limit = min(s.len, a.max_kv);
+    return s;
+}
+// Keys that query i sees.
+__device__ inline int visible(const Attention &a, const Sequence &s, int i) { return a.causal ? min(max(s.len - s.total + i + 1, 0), s.limit) : s.limit; }
+
+// ---- how rows lie in LDS
+template <int D>
+struct Rows {
+    static constexpr int kBytes = 2 * D, kPieces = D / 8, kPerTransfer = 64 / kPieces;      // rows that one transfer of a wave brings
+    // Place of piece c of a row: of keys, 32 rows are read at one piece; of values, four rows at four pieces
+    __device__ static int key_piece(int row, int c) { return D == 128 ? c ^ (row & 15) : c ^ (row >> 1 & 7); }
+    __device__ static int value_piece(int row, int c) { return D == 128 ? c ^ (row & 3) << 2 : c ^ (row >> 1 & 1) << 2; }
+};
+
+template <int D>
+struct Wave {
+    typedef Rows<D> R;
+    static constexpr int kSteps = D / 16, kTiles = D / 32;
+    Operand q[kSteps];
+    float16v o[kTiles];
+    float top, sum;
+    int lane, half, end;            // keys that the lane's row sees
+
+    __device__ void begin(const Cut &w, const Sequence &s, int head, int row, int rows, int lane_)
+    {
+        lane = lane_;
+        half = lane >> 5;
+        top = kNone;
+        sum = 0.0f;
+        end = row < rows ? visible(w.a, s, row / w.group) : 0;
+        const int r = min(row, rows - 1), i = r / w.group;
+        const uint16_t *const from = w.a.q + (long long)(s.q0 + i) * w.a.q_stride + (head * w.group + r - i * w.group) * D + 8 * half;
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+            q[k].u = *reinterpret_cast<const uint4 *>(from + 16 * k);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) q[k].w[j] = (q[k].w[j] & w.keep) ^ w.flip;
+        }
+#pragma unroll
+        for (int c = 0; c < kTiles; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[c][i] = 0.0f;
+    }
+    // scores of 32 keys at `keys` (LDS)
+    __device__ float16v scores(const char *keys) const
+    {
+        float16v x;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = 0.0f;
+        const int row = lane & 31;
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+            Operand a;
+            a.u = *reinterpret_cast<const uint4 *>(keys + row * R::kBytes + R::key_piece(row, 2 * k + half) * 16);
+            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.b, q[k].b, x, 0, 0, 0);
+        }
+        return x;
+    }
+    // Unseen keys of NK x 32 from number t on.
+    template <int NK>
+    __device__ void hide(float16v (&x)[NK], int t) const
+    {
+        const int seen = end - t - 4 * half;
+#pragma unroll
+        for (int k = 0; k < NK; ++k)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[k][i] = 32 * k + 8 * (i / 4) + i % 4 < seen ? x[k][i] : -INFINITY;
+    }
+    // Weights of NK x 32 keys, as operands of 16 keys each.
+    template <int NK>
+    __device__ void weights(const float16v (&x)[NK], float scale2, Operand (&p)[2 * NK])
+    {
+        float m = fmaxf(x[0][0], x[0][1]);
+#pragma unroll
+        for (int k = 0; k < NK; ++k)
+#pragma unroll
+            for (int i = k == 0 ? 2 : 0; i < 16; i += 2) m = fmaxf(fmaxf(m, x[k][i]), x[k][i + 1]);
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+        m = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+        if (__builtin_amdgcn_ballot_w64((m - top) * scale2 > kSlack)) {
+            const float next = fmaxf(top, m), f = __builtin_amdgcn_exp2f((top - next) * scale2);
+            top = next;
+            sum *= f;
+#pragma unroll
+            for (int c = 0; c < kTiles; ++c)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[c][i] *= f;
+        }
+        const float off = top * scale2;
+        bf16x2 one;
+        one[0] = one[1] = (__bf16)1.0f;
+#pragma unroll
+        for (int k = 0; k < NK; ++k)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const float a = __builtin_amdgcn_exp2f(fmaf(x[k][i], scale2, -off)), b = __builtin_amdgcn_exp2f(fmaf(x[k][i + 1], scale2, -off));
+                const uint32_t both = pack_bf16x2(a, b);
+                p[2 * k + i / 8].w[i % 8 / 2] = both;
+                sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, both), one, sum, false);
+            }
+    }
+    // 16 keys' values at `values` (LDS)
+    __device__ void add(const char *values, const Operand &p)
+    {
+        const int i = lane & 15, row = 4 * half + (i >> 2);
+#pragma unroll
+        for (int c = 0; c < kTiles; ++c) {
+            const int piece = R::value_piece(row, 4 * c + 2 * (lane >> 4 & 1) + (i >> 1 & 1));
+            const char *const at = values + row * R::kBytes + piece * 16 + 8 * (i & 1);
+            Operand a;
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                a.s[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v *)(const_cast<char *>(at) + 8 * j * R::kBytes));
+            o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.b, p.b, o[c], 0, 0, 0);
+        }
+    }
+    // A value that is no number touches only the rows that see it: where `keys` rows of values have one and some rows of the wave do not see all of those keys, it is added to the rows that
+    // do, here, before it is taken out of LDS.  A weight is never 0, so an infinity stays one.
+    __device__ void add_no_numbers(const char *values, int t, int keys)
+    {
+        for (int key = 0; key < keys; ++key)
+#pragma unroll
+            for (int c = 0; c < kTiles; ++c)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const uint2 v = *reinterpret_cast<const uint2 *>(values + key * R::kBytes + R::value_piece(key, 4 * c + g) * 16 + 8 * half);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t bits = (i & 2 ? v.y : v.x) >> 16 * (i & 1) << 16;
+                        if ((bits & 0x7f800000u) == 0x7f800000u && t + key < end) o[c][4 * g + i] += __uint_as_float(bits);
+                    }
+                }
+    }
+    // A row's parts of the two lanes that have it.
+    __device__ float total() const
+    {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+        return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+};
+
+// Whether 16 bytes have a bf16 infinity or NaN in them; the same without those.
+__device__ inline bool no_numbers(const uint4 &v)
+{
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w = i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
+        bad |= (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+    }
+    return bad;
+}
+__device__ inline uint32_t numbers_of(uint32_t w) { return w & ((w & 0x7f80u) == 0x7f80u ? 0xffff0000u : 0xffffffffu) & ((w & 0x7f800000u) == 0x7f800000u ? 0x0000ffffu : 0xffffffffu); }
+// Pieces first, first + step, ... of `bytes` at `values`: whether there is one with no numbers, and taking those out.
+__device__ inline bool find_no_numbers(const char *values, int bytes, int first, int step)
+{
+    bool bad = false;
+    for (int at = 16 * first; at < bytes; at += 16 * step) bad |= no_numbers(*reinterpret_cast<const uint4 *>(values + at));
+    return bad;
+}
+__device__ inline void take_out_no_numbers(char *values, int bytes, int first, int step)
+{
+    for (int at = 16 * first; at < bytes; at += 16 * step) {
+        uint4 &v = *reinterpret_cast<uint4 *>(values + at);
+        if (no_numbers(v)) v = make_uint4(numbers_of(v.x), numbers_of(v.y), numbers_of(v.z), numbers_of(v.w));
+    }
+}
+
+// ---- from memory into LDS
+__device__ inline uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)p; }
+// One transfer: rows first .. first + kPerTransfer - 1 of those at `from` (rows past `most` are read as that one), to `lds` + their place
+template <int D, bool KEYS>
+__device__ inline void transfer(const uint16_t *from, long long stride, int first, int most, uint32_t lds, int lane)
+{
+    typedef Rows<D> R;
+    const int row = first + lane / R::kPieces, c = lane % R::kPieces;
+    const int piece = KEYS ? R::key_piece(row, c) : R::value_piece(row, c);
+    dma16((uint32_t)(min(row, most) * (int)stride * 2 + piece * 16), from, lds + first * R::kBytes);
+}
+
+template <int D>
+constexpr int kPartial = D + 2;
+__device__ inline size_t partial_row(const Cut &w, int b, int head, int row, int split)
+{
+    return (((size_t)b * w.a.kv_heads + head) * ((size_t)w.a.max_q * w.group) + row) * w.splits + split;
+}
+
+// ---- many rows: a wave has 32 of its own, the four waves of a block go through the same keys
+template <int D>
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attention_own_rows_kernel(Cut w)
+{
+    typedef Rows<D> R;
+    constexpr int kKeys = 64, kTile = kKeys * R::kBytes;
+    __shared__ __align__(16) char keys[2][kTile], values[2][kTile];
+    const Attention &a = w.a;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // Heads first, parts next, then tiles from the last one on, where rows see most, sequences last: blocks that run together have keys in common (those of a head on one of the eight dies, where
+    // heads are a multiple of eight), and a sequence's longest blocks begin first
+    const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, place = rest % (w.tiles * w.splits), b = rest / (w.tiles * w.splits);
+    const Sequence seq = sequence_of(a, b);
+    const int rows = seq.n * w.group, tile = (rows + 127) / 128 - 1 - place / w.splits, split = place % w.splits;
+    if (tile < 0) return;
+    const int row0 = tile * 128, row = row0 + 32 * wave + (lane & 31), rows_end = min(rows, row0 + 128);
+    const int last = visible(a, seq, (rows_end - 1) / w.group), full = visible(a, seq, row0 / w.group);        // keys that some row of the block sees, and that all see
+    const int t0 = split * w.chunk, stop = min(last, t0 + w.chunk);
+    if (split > 0 && t0 >= last) return;
+    Wave<D> r;
+    r.begin(w, seq, head, row, rows, lane);
+    const uint16_t *const k = a.k + (long long)seq.k0 * a.k_stride + head * D, *const v = a.v + (long long)seq.k0 * a.v_stride + head * D;
+    auto bring = [&](int t, int buffer) {
+        const uint16_t *const from_k = k + (long long)t * a.k_stride, *const from_v = v + (long long)t * a.v_stride;
+        constexpr int kEach = kKeys / R::kPerTransfer / 4;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) transfer<D, true>(from_k, a.k_stride, (wave * kEach + i) * R::kPerTransfer, last - 1 - t, lds_address(keys[buffer]), lane);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) transfer<D, false>(from_v, a.v_stride, (wave * kEach + i) * R::kPerTransfer, last - 1 - t, lds_address(values[buffer]), lane);
+    };
+    if (t0 < stop) bring(t0, 0);
+    int buffer = 0;
+    for (int t = t0; t < stop; t += kKeys, buffer ^= 1) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();                                    // the tile is there, and nobody reads the other buffer any more
+        if (t + kKeys < stop) bring(t + kKeys, buffer ^ 1);
+        float16v x[2];
+        Operand p[4];
+        x[0] = r.scores(keys[buffer]);
+        x[1] = r.scores(keys[buffer] + 32 * R::kBytes);
+        if (t + kKeys > full) {
+            r.hide(x, t);
+            if (__syncthreads_or(find_no_numbers(values[buffer], kTile, threadIdx.x, 256))) {
+                r.weights(x, w.scale2, p);
+                r.add_no_numbers(values[buffer], t, kKeys);
+                __syncthreads();
+                take_out_no_numbers(values[buffer], kTile, threadIdx.x, 256);
+                __syncthreads();
+            } else r.weights(x, w.scale2, p);
+        } else r.weights(x, w.scale2, p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.add(values[buffer] + 16 * i * R::kBytes, p[i]);
+    }
+    const float total = r.total();
+    if (row >= rows) return;
+    if (w.splits == 1) {
+        const float f = total != 0.0f ? 1.0f / total : 0.0f;        // (a row that is no number has a total that is none)
+        const int i = row / w.group;
+        uint16_t *const to = a.out + ((long long)(seq.q0 + i) * a.q_heads + head * w.group + row - i * w.group) * D;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<uint2 *>(to + 32 * c + 8 * g + 4 * r.half) =
+                    make_uint2(pack_bf16x2(r.o[c][4 * g] * f, r.o[c][4 * g + 1] * f), pack_bf16x2(r.o[c][4 * g + 2] * f, r.o[c][4 * g + 3] * f));
+    } else {
+        float *const to = w.partials + partial_row(w, b, head, row, split) * kPartial<D>;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+#pragma unroll
+                for (int i = 0; i < 4; i += 2)
+                    *reinterpret_cast<float2 *>(to + 32 * c + 8 * g + 4 * r.half + i) = make_float2(r.o[c][4 * g + i], r.o[c][4 * g + i + 1]);
+        if (r.half == 0) *reinterpret_cast<float2 *>(to + D) = make_float2(r.top * w.scale2, total);
+    }
+}
+
+// ---- few rows (32 at most): the waves of a block share them and go through keys of their own, 32 at a time, brought into LDS by each for itself
+template <int D>
+__global__ __launch_bounds__(256, 2) void attention_few_rows_kernel(Cut w)
+{
+    typedef Rows<D> R;
+    constexpr int kKeys = 32, kTile = kKeys * R::kBytes, kEach = kKeys / R::kPerTransfer;
+    __shared__ __align__(16) char area[4][2][kTile];
+    __shared__ float tops[4][32], totals[4][32];
+    const Attention &a = w.a;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, split = rest % w.splits, b = rest / w.splits;
+    const Sequence seq = sequence_of(a, b);
+    const int rows = seq.n * w.group;
+    if (rows == 0) return;
+    const int last = visible(a, seq, seq.n - 1), full = visible(a, seq, 0), t0 = split * w.chunk, stop = min(last, t0 + w.chunk);
+    if (split > 0 && t0 >= last) return;
+    Wave<D> r;
+    const uint16_t *const k = a.k + (long long)seq.k0 * a.k_stride + head * D, *const v = a.v + (long long)seq.k0 * a.v_stride + head * D;
+    char *const keys = area[wave][0], *const values = area[wave][1];
+    auto bring_keys = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) transfer<D, true>(k + (long long)t * a.k_stride, a.k_stride, i * R::kPerTransfer, last - 1 - t, lds_address(keys), lane);
+    };
+    auto bring_values = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) transfer<D, false>(v + (long long)t * a.v_stride, a.v_stride, i * R::kPerTransfer, last - 1 - t, lds_address(values), lane);
+    };
+    r.begin(w, seq, head, lane & 31, rows, lane);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // the queries: from here on only transfers are counted
+    int t = t0 + kKeys * wave;
+    if (t < stop) {
+        bring_keys(t);
+        bring_values(t);
+    }
+    for (; t < stop; t += 4 * kKeys) {
+        const bool more = t + 4 * kKeys < stop;
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kEach) : "memory");        // the keys; the values are on their way
+        lanes_exchange_fence();
+        float16v x[1];
+        Operand p[2];
+        x[0] = r.scores(keys);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (more) bring_keys(t + 4 * kKeys);
+        const bool masked = t + kKeys > full;
+        if (masked) r.hide(x, t);
+        r.weights(x, w.scale2, p);
+        if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kEach) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        lanes_exchange_fence();
+        if (masked && __builtin_amdgcn_ballot_w64(find_no_numbers(values, kTile, lane, 64))) {
+            r.add_no_numbers(values, t, kKeys);
+            lanes_exchange_fence();
+            take_out_no_numbers(values, kTile, lane, 64);
+            lanes_exchange_fence();
+        }
+        r.add(values, p[0]);
+        r.add(values + 16 * R::kBytes, p[1]);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (more) bring_values(t + 4 * kKeys);
+    }
+    // The waves' sums, in the LDS that held their tiles: rows of D floats, their pieces of four in an order by the row
+    const float total = r.total();
+    __syncthreads();
+    constexpr int kFours = D / 4;
+    float *const mine = reinterpret_cast<float *>(area[wave][0]);
+    const int here = lane & 31;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<float4 *>(mine + here * D + ((8 * c + 2 * g + r.half) ^ (here & (kFours - 1))) * 4) =
+                make_float4(r.o[c][4 * g], r.o[c][4 * g + 1], r.o[c][4 * g + 2], r.o[c][4 * g + 3]);
+    if (lane < 32) {
+        tops[wave][lane] = r.top;
+        totals[wave][lane] = total;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < rows * kFours; i += 256) {
+        const int row = i / kFours, c = i % kFours;
+        float top = kNone, all = 0.0f;
+#pragma unroll
+        for (int n = 0; n < 4; ++n) top = fmaxf(top, tops[n][row]);
+        float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            const float f = __builtin_amdgcn_exp2f((tops[n][row] - top) * w.scale2);
+            const float4 y = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(area[n][0]) + row * D + (c ^ (row & (kFours - 1))) * 4);
+            all = fmaf(f, totals[n][row], all);
+            x = make_float4(fmaf(f, y.x, x.x), fmaf(f, y.y, x.y), fmaf(f, y.z, x.z), fmaf(f, y.w, x.w));
+        }
+        if (w.splits == 1) {
+            const float f = all != 0.0f ? 1.0f / all : 0.0f;
+            const int at = row / w.group;
+            *reinterpret_cast<uint2 *>(a.out + ((long long)(seq.q0 + at) * a.q_heads + head * w.group + row - at * w.group) * D + 4 * c) =
+                make_uint2(pack_bf16x2(x.x * f, x.y * f), pack_bf16x2(x.z * f, x.w * f));
+        } else {
+            float *const to = w.partials + partial_row(w, b, head, row, split) * kPartial<D>;
+            *reinterpret_cast<float2 *>(to + 4 * c) = make_float2(x.x, x.y);
+            *reinterpret_cast<float2 *>(to + 4 * c + 2) = make_float2(x.z, x.w);
+            if (c == 0) *reinterpret_cast<float2 *>(to + D) = make_float2(top * w.scale2, all);
+        }
+    }
+}
+
+// ---- the parts of a row put together: 16 lanes have a row
+template <int D>
+__global__ __launch_bounds__(256) void attention_join_kernel(Cut w)
+{
+    constexpr int C = D / 16;
+    const Attention &a = w.a;
+    const int first = (threadIdx.x & 15) * C, blocks = (a.max_q * w.group + 15) / 16;
+    const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, b = rest / blocks, row = rest % blocks * 16 + (threadIdx.x >> 4);
+    const Sequence seq = sequence_of(a, b);
+    if (row >= seq.n * w.group) return;
+    const int i = row / w.group, used = (visible(a, seq, i) + w.chunk - 1) / w.chunk;
+    const float *const from = w.partials + partial_row(w, b, head, row, 0) * kPartial<D>;
+    float top = kNone, total = 0.0f, x[C];
+    for (int s = 0; s < used; ++s) top = fmaxf(top, from[(size_t)s * kPartial<D> + D]);
+#pragma unroll
+    for (int c = 0; c < C; ++c) x[c] = 0.0f;
+    for (int s = 0; s < used; ++s) {
+        const float *const p = from + (size_t)s * kPartial<D>;
+        const float f = __builtin_amdgcn_exp2f(p[D] - top);
+        total = fmaf(f, p[D + 1], total);
+#pragma unroll
+        for (int c = 0; c < C; ++c) x[c] = fmaf(f, p[first + c], x[c]);
+    }
+    const float f = total != 0.0f ? 1.0f / total : 0.0f;
+    uint32_t *const to = reinterpret_cast<uint32_t *>(a.out + ((long long)(seq.q0 + i) * a.q_heads + head * w.group + row - i * w.group) * D + first);
+#pragma unroll
+    for (int c = 0; c < C; c += 2) to[c / 2] = pack_bf16x2(x[c] * f, x[c + 1] * f);
+}
+
+template <int D>
+hipError_t launch(const Attention &a, hipStream_t stream)
+{
+    const int group = a.q_heads / a.kv_heads;
+    const AttentionPlan p = attention_plan(a.seqs, a.max_q, a.max_kv, a.q_heads, a.kv_heads, D);
+    const Cut w{a, group, p.chunk, p.splits, p.tiles, a.scale == 0.0f ? 1.0f : __builtin_fabsf(a.scale) * kLog2e, a.scale < 0.0f ? 0x80008000u : 0u, a.scale == 0.0f ? 0u : 0xffffffffu,
+                static_cast<float *>(a.workspace)};
+    const dim3 grid((unsigned)a.seqs * a.kv_heads * p.tiles * p.splits);
+    if (p.few) attention_few_rows_kernel<D><<<grid, 256, 0, stream>>>(w);
+    else attention_own_rows_kernel<D><<<grid, 256, 0, stream>>>(w);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.splits == 1) return e;
+    attention_join_kernel<D><<<dim3((unsigned)a.seqs * a.kv_heads * ((a.max_q * group + 15) / 16)), 256, 0, stream>>>(w);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t run_attention(const Attention &a, int d, hipStream_t stream) { return d == 64 ? launch<64>(a, stream) : launch<128>(a, stream); }
+
+}  // namespace qvggt

@@ -1,0 +1,92 @@
+// The row operators around a block's layers: heads of queries and keys normalised and rotated, and the residual stream's update with its norms.
+#pragma once
+#include <type_traits>
+
+#include "qvggt_common.h"
+
+namespace qvggt {
+
+enum { kNormNone = 0, kNormLayer = 1, kNormRms = 2 };
+
+struct HeadsNormRope {
+    const void *in[2];              // queries, keys
+    void *out[2];
+    long long in_stride[2], out_stride[2];
+    int heads[2];
+    const float *gain[2], *bias[2];
+    int T, f32, norm;
+    float eps;
+    const float *rope;              // [rows][cosines dim / 2, sines dim / 2], or nullptr
+    int rows, dim, pair, axes;
+    const int32_t *positions;       // [axes][T]
+    const uint8_t *pair_axis;       // [dim / 2], or nullptr: axis p * axes / (dim / 2)
+};
+hipError_t run_heads_norm_rope(const HeadsNormRope &a, int d, hipStream_t stream);
+
+struct ResidualNorm {
+    const void *x, *y;
+    int x_f32, y_f32, M, C, post_norm;
+    const float *post_gain, *post_bias, *scale;
+    const void *gate;
+    int norm;
+    const float *gain, *bias;
+    const void *mod_scale, *mod_shift;
+    int cond_f32, cond_rows;
+    long long cond_stride;
+    const int32_t *row_of;
+    float eps;
+    void *x_out, *h;
+    int h_f32;
+};
+hipError_t run_residual_norm(const ResidualNorm &a, hipStream_t stream);
+
+// ---- eight consecutive channels of a row
+struct Eight {
+    uint32_t w[8];                  // bf16: half of them
+
+    __device__ void load(const void *row, bool f32, int first)
+    {
+        if (f32) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint4 v = reinterpret_cast<const uint4 *>(static_cast<const float *>(row) + first)[i];
+                w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+            }
+        } else {
+            const uint4 v = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(row) + first);
+            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+        }
+    }
+    __device__ void floats(bool f32, float (&y)[8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = f32 ? __uint_as_float(w[i]) : __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    }
+};
+__device__ inline void store_eight(void *row, bool f32, int first, const float (&y)[8])
+{
+    if (f32) {
+        float4 *const to = reinterpret_cast<float4 *>(static_cast<float *>(row) + first);
+        to[0] = make_float4(y[0], y[1], y[2], y[3]);
+        to[1] = make_float4(y[4], y[5], y[6], y[7]);
+    } else
+        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(row) + first) = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
+}
+__device__ inline void load_eight(const float *from, float (&y)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float4 v = reinterpret_cast<const float4 *>(from)[i];
+        y[4 * i] = v.x; y[4 * i + 1] = v.y; y[4 * i + 2] = v.z; y[4 * i + 3] = v.w;
+    }
+}
+
+// 1 / sqrt(v).  The instruction takes a number below 2^-126 for 0; those, and some more, are lifted first.
+__device__ inline float inverse_root(float v)
+{
+    const bool low = v < 0x1p-100f;
+    const float r = __builtin_amdgcn_rsqf(low ? v * 0x1p100f : v);
+    return low ? r * 0x1p50f : r;
+}
+
+}  // namespace qvggt
