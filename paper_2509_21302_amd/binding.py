@@ -61,6 +61,7 @@ NORMS = ("none", "layer", "rms")
 
 # ... and those that its functions of their own call, in its order
 KV4 = ("qvggt_kv4_append", "qvggt_kv4_read", "qvggt_kv4_attention")
+BLOCK = ("qvggt_heads_norm_rope", "qvggt_attention", "qvggt_residual_norm")
 
 
 class QvggtError(RuntimeError):
@@ -231,6 +232,8 @@ def load_library() -> C.CDLL:
             _call.bind(kind, C.cast(getattr(lib, name), C.c_void_p).value)
         for which, name in enumerate(KV4):
             _call.bind_kv4(which, C.cast(getattr(lib, name), C.c_void_p).value)
+        for which, name in enumerate(BLOCK):
+            _call.bind_block(which, C.cast(getattr(lib, name), C.c_void_p).value)
     _lib = lib
     return lib
 
@@ -793,6 +796,9 @@ def _here(where, *tensors):
 def qvggt_heads_norm_rope(Q, K, Q_out, K_out, norm="none", eps=1e-6, q_gain=None, q_bias=None, k_gain=None, k_bias=None, rope=None, positions=None, rope_pair=0, pair_axis=None,
                           stream=None):
     """Q [T, q_heads, d] and K [T, kv_heads, d] (either may be None, with its output) into Q_out and K_out, which may be the same tensors."""
+    if stream is None and _call is not None and _native(_call.heads_norm_rope, "qvggt_heads_norm_rope", Q, K, Q_out, K_out, norm, eps, q_gain, q_bias, k_gain, k_bias, rope, positions, rope_pair,
+                                                        pair_axis):
+        return
     some = Q if Q is not None else K
     T, _, d = some.shape
     heads, at, strides, outs, out_strides = [], [], [], [], []
@@ -832,6 +838,8 @@ def qvggt_attention_workspace_bytes(T: int, seqs: int, max_q: int, max_kv: int, 
 
 def qvggt_attention(Q, K, V, scale, causal, q_starts, kv_starts, kv_lens, max_q, max_kv, out, workspace, stream=None):
     """Q [T, q_heads, d], K and V [S, kv_heads, d], out [T, q_heads, d], all bf16; q_starts int32 [seqs + 1]; kv_starts int32 [seqs + 1] with kv_lens None, both [seqs] otherwise."""
+    if stream is None and _call is not None and _native(_call.attention, "qvggt_attention", Q, K, V, scale, causal, q_starts, kv_starts, kv_lens, max_q, max_kv, out, workspace):
+        return
     T, heads, d = Q.shape
     S, kv_heads, _ = K.shape
     if V.shape != K.shape or K.shape[2] != d or not Q.dtype == K.dtype == V.dtype:
@@ -854,6 +862,9 @@ def qvggt_attention(Q, K, V, scale, causal, q_starts, kv_starts, kv_lens, max_q,
 def qvggt_residual_norm(x, y, x_out, h, post_norm="none", post_gain=None, post_bias=None, scale=None, gate=None, norm="none", gain=None, bias=None, mod_scale=None, mod_shift=None,
                         row_of=None, eps=1e-6, stream=None):
     """x and y [M, C] (y may be None), x_out of x's type and h [M, C] (either may be None); gate, mod_scale and mod_shift [rows, C], of one type and with one distance between rows."""
+    if stream is None and _call is not None and _native(_call.residual_norm, "qvggt_residual_norm", x, y, x_out, h, post_norm, post_gain, post_bias, scale, gate, norm, gain, bias, mod_scale,
+                                                        mod_shift, row_of, eps):
+        return
     M, C = x.shape
     for t, name in ((y, "y"), (x_out, "x_out"), (h, "h")):
         if t is not None and t.shape != x.shape:

@@ -11,6 +11,8 @@
 //
 // The running maximum of a row is raised when one of its scores exceeds it by more than 2^8 in weight: weights are at most 2^8 then, and sums are multiplied by a factor in few steps.  Weights
 // are rounded to bf16 (to nearest), for the product and for the sum that it is divided by alike.  A row starts from a maximum of -3e38, so that rows that see nothing end with a sum of 0.
+#include <type_traits>
+
 #include "attention.h"
 #include "attention_plan.h"
 #include "lds_transfer.h"
@@ -97,20 +99,19 @@ struct Wave {
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[c][i] = 0.0f;
     }
-    // scores of 32 keys at `keys` (LDS)
-    __device__ float16v scores(const char *keys) const
+    // Scores of NK x 32 keys at `keys` (LDS).
+    template <int NK>
+    __device__ void scores(const char *keys, float16v (&x)[NK]) const
     {
-        float16v x;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = 0.0f;
         const int row = lane & 31;
 #pragma unroll
-        for (int k = 0; k < kSteps; ++k) {
-            Operand a;
-            a.u = *reinterpret_cast<const uint4 *>(keys + row * R::kBytes + R::key_piece(row, 2 * k + half) * 16);
-            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.b, q[k].b, x, 0, 0, 0);
-        }
-        return x;
+        for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+            for (int n = 0; n < NK; ++n) {
+                Operand a;
+                a.u = *reinterpret_cast<const uint4 *>(keys + (row * R::kBytes + R::key_piece(row, 2 * k + half) * 16) + 32 * n * R::kBytes);
+                x[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.b, q[k].b, k == 0 ? float16v{} : x[n], 0, 0, 0);
+            }
     }
     // Unseen keys of NK x 32 from number t on.
     template <int NK>
@@ -122,9 +123,9 @@ struct Wave {
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[k][i] = 32 * k + 8 * (i / 4) + i % 4 < seen ? x[k][i] : -INFINITY;
     }
-    // Weights of NK x 32 keys, as operands of 16 keys each.
+    // The largest score of a row.
     template <int NK>
-    __device__ void weights(const float16v (&x)[NK], float scale2, Operand (&p)[2 * NK])
+    __device__ static float largest(const float16v (&x)[NK])
     {
         float m = fmaxf(x[0][0], x[0][1]);
 #pragma unroll
@@ -132,7 +133,11 @@ struct Wave {
 #pragma unroll
             for (int i = k == 0 ? 2 : 0; i < 16; i += 2) m = fmaxf(fmaxf(m, x[k][i]), x[k][i + 1]);
         const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
-        m = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+        return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    // ... and the maximum raised to it where that is called for.
+    __device__ void raise(float m, float scale2)
+    {
         if (__builtin_amdgcn_ballot_w64((m - top) * scale2 > kSlack)) {
             const float next = fmaxf(top, m), f = __builtin_amdgcn_exp2f((top - next) * scale2);
             top = next;
@@ -142,6 +147,11 @@ struct Wave {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[c][i] *= f;
         }
+    }
+    // Weights of NK x 32 keys, as operands of 16 keys each.
+    template <int NK>
+    __device__ void weights(const float16v (&x)[NK], float scale2, Operand (&p)[2 * NK])
+    {
         const float off = top * scale2;
         bf16x2 one;
         one[0] = one[1] = (__bf16)1.0f;
@@ -241,13 +251,36 @@ __device__ inline size_t partial_row(const Cut &w, int b, int head, int row, int
     return (((size_t)b * w.a.kv_heads + head) * ((size_t)w.a.max_q * w.group) + row) * w.splits + split;
 }
 
+// The order in which a step's instructions are issued: vector instructions and LDS reads between the products, evenly (13740 rows on as many keys, 64 channels: 871 us, 898 in the compiler's own order;
+// a prompt of 11003, 128 channels: 911 and 918).
+template <int D>
+__device__ inline void pace()
+{
+    constexpr int kProducts = D / 8, kBetween = 512 / D;
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+    for (int i = 0; i < kProducts; ++i) {                   // scores: a product, vector instructions, a read of keys
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x2, kBetween, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < kProducts; ++i) {                   // results: two reads of values, a product, vector instructions
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x2, kBetween, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // ---- many rows: a wave has 32 of its own, the four waves of a block go through the same keys
 template <int D>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attention_own_rows_kernel(Cut w)
 {
     typedef Rows<D> R;
-    constexpr int kKeys = 64, kTile = kKeys * R::kBytes;
-    __shared__ __align__(16) char keys[2][kTile], values[2][kTile];
+    constexpr int kKeys = 64, kTile = kKeys * R::kBytes, kEach = kKeys / R::kPerTransfer / 4;
+    __shared__ __align__(16) char area[4 * kTile];          // two tiles of keys, two of values
+    char *const keys = area, *const values = area + 2 * kTile;
     const Attention &a = w.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // Heads first, parts next, then tiles from the last one on, where rows see most, sequences last: blocks that run together have keys in common (those of a head on one of the eight dies, where
@@ -258,41 +291,110 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attention_own_rows_kerne
     if (tile < 0) return;
     const int row0 = tile * 128, row = row0 + 32 * wave + (lane & 31), rows_end = min(rows, row0 + 128);
     const int last = visible(a, seq, (rows_end - 1) / w.group), full = visible(a, seq, row0 / w.group);        // keys that some row of the block sees, and that all see
-    const int t0 = split * w.chunk, stop = min(last, t0 + w.chunk);
+    const int t0 = split * w.chunk, stop = min(last, t0 + w.chunk), steps = (stop - t0 + kKeys - 1) / kKeys;
     if (split > 0 && t0 >= last) return;
     Wave<D> r;
     r.begin(w, seq, head, row, rows, lane);
-    const uint16_t *const k = a.k + (long long)seq.k0 * a.k_stride + head * D, *const v = a.v + (long long)seq.k0 * a.v_stride + head * D;
-    auto bring = [&](int t, int buffer) {
-        const uint16_t *const from_k = k + (long long)t * a.k_stride, *const from_v = v + (long long)t * a.v_stride;
-        constexpr int kEach = kKeys / R::kPerTransfer / 4;
+    const uint16_t *const k = a.k + (long long)(seq.k0 + t0) * a.k_stride + head * D, *const v = a.v + (long long)(seq.k0 + t0) * a.v_stride + head * D;
+    // A lane's place in this wave's transfers of a tile: the keys' pieces change with the row, the values' do not from transfer to transfer
+    uint32_t from_key[kEach], from_value;
+    const int row_of_lane = lane / R::kPieces, piece = lane % R::kPieces, first = wave * kEach * R::kPerTransfer;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) transfer<D, true>(from_k, a.k_stride, (wave * kEach + i) * R::kPerTransfer, last - 1 - t, lds_address(keys[buffer]), lane);
+    for (int i = 0; i < kEach; ++i) {
+        const int at = first + i * R::kPerTransfer + row_of_lane;
+        from_key[i] = (uint32_t)(at * (int)a.k_stride * 2 + R::key_piece(at, piece) * 16);
+    }
+    from_value = (uint32_t)((first + row_of_lane) * (int)a.v_stride * 2 + R::value_piece(first + row_of_lane, piece) * 16);
+    const uint32_t lds = lds_address(area) + first * R::kBytes;
+    auto bring_keys = [&](int step, int buffer) {
+        const uint16_t *const from = k + (long long)step * kKeys * a.k_stride;
+        const uint32_t to = lds + buffer * kTile;
+        if (t0 + (step + 1) * kKeys <= last) {
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) transfer<D, false>(from_v, a.v_stride, (wave * kEach + i) * R::kPerTransfer, last - 1 - t, lds_address(values[buffer]), lane);
+            for (int i = 0; i < kEach; ++i) dma16(from_key[i], from, to + i * R::kPerTransfer * R::kBytes);
+        } else
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) transfer<D, true>(from, a.k_stride, first + i * R::kPerTransfer, last - 1 - t0 - step * kKeys, lds_address(keys) + buffer * kTile, lane);
     };
-    if (t0 < stop) bring(t0, 0);
-    int buffer = 0;
-    for (int t = t0; t < stop; t += kKeys, buffer ^= 1) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();                                    // the tile is there, and nobody reads the other buffer any more
-        if (t + kKeys < stop) bring(t + kKeys, buffer ^ 1);
-        float16v x[2];
-        Operand p[4];
-        x[0] = r.scores(keys[buffer]);
-        x[1] = r.scores(keys[buffer] + 32 * R::kBytes);
-        if (t + kKeys > full) {
-            r.hide(x, t);
-            if (__syncthreads_or(find_no_numbers(values[buffer], kTile, threadIdx.x, 256))) {
-                r.weights(x, w.scale2, p);
-                r.add_no_numbers(values[buffer], t, kKeys);
-                __syncthreads();
-                take_out_no_numbers(values[buffer], kTile, threadIdx.x, 256);
-                __syncthreads();
-            } else r.weights(x, w.scale2, p);
-        } else r.weights(x, w.scale2, p);
+    auto bring_values = [&](int step, int buffer) {
+        const uint16_t *const from = v + (long long)step * kKeys * a.v_stride;
+        const uint32_t to = lds + (2 + buffer) * kTile;
+        if (t0 + (step + 1) * kKeys <= last) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r.add(values[buffer] + 16 * i * R::kBytes, p[i]);
+            for (int i = 0; i < kEach; ++i) dma16(from_value, from + (long long)i * R::kPerTransfer * a.v_stride, to + i * R::kPerTransfer * R::kBytes);
+        } else
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) transfer<D, false>(from, a.v_stride, first + i * R::kPerTransfer, last - 1 - t0 - step * kKeys, lds_address(values) + buffer * kTile, lane);
+    };
+    auto arrived = [] {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    };
+    if (steps > 0) {
+        // While a step's weights are made the next one's scores are multiplied, and its maximum is looked for while this one's values are: keys are a step ahead of values
+        float16v x[2], y[2];
+        Operand p[4];
+        bring_keys(0, 0);
+        bring_values(0, 0);
+        arrived();
+        r.scores(keys, x);
+        if (steps > 1) bring_keys(1, 1);
+        float m = r.largest(x);
+        arrived();
+        // Steps that every row of the block sees, two at a time; behind each of them there is another
+        const int plain = min(max(full - t0, 0) / kKeys, steps - 1) & ~1;
+        int step = 0;
+        auto both = [&](auto parity, float16v(&x)[2], float16v(&y)[2]) {
+            constexpr int kHere = decltype(parity)::value, kNext = kHere ^ 1;
+            if (step + 2 < steps) bring_keys(step + 2, kHere);
+            bring_values(step + 1, kNext);
+            r.raise(m, w.scale2);
+            r.scores(keys + kNext * kTile, y);
+            r.weights(x, w.scale2, p);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r.add(values + kHere * kTile + 16 * i * R::kBytes, p[i]);
+            m = r.largest(y);
+            ++step;
+            pace<D>();
+            arrived();
+        };
+        while (step < plain) {
+            both(std::integral_constant<int, 0>(), x, y);
+            both(std::integral_constant<int, 1>(), y, x);
+        }
+        for (; step < steps; ++step) {
+            const int here = step & 1;
+            const bool more = step + 1 < steps;
+            if (step + 2 < steps) bring_keys(step + 2, here);
+            if (more) {
+                bring_values(step + 1, here ^ 1);
+                r.scores(keys + (here ^ 1) * kTile, y);
+            }
+            const int t = t0 + step * kKeys;
+            char *const mine = values + here * kTile;
+            bool bad = false;
+            if (t + kKeys > full) {
+                r.hide(x, t);
+                m = r.largest(x);
+                bad = __syncthreads_or(find_no_numbers(mine, kTile, threadIdx.x, 256));
+            }
+            r.raise(m, w.scale2);
+            r.weights(x, w.scale2, p);
+            if (bad) {
+                r.add_no_numbers(mine, t, kKeys);
+                __syncthreads();
+                take_out_no_numbers(mine, kTile, threadIdx.x, 256);
+                __syncthreads();
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r.add(mine + 16 * i * R::kBytes, p[i]);
+            if (more) {
+                x[0] = y[0];
+                x[1] = y[1];
+                m = r.largest(x);
+            }
+            arrived();
+        }
     }
     const float total = r.total();
     if (row >= rows) return;
@@ -359,11 +461,12 @@ __global__ __launch_bounds__(256, 2) void attention_few_rows_kernel(Cut w)
         lanes_exchange_fence();
         float16v x[1];
         Operand p[2];
-        x[0] = r.scores(keys);
+        r.scores(keys, x);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (more) bring_keys(t + 4 * kKeys);
         const bool masked = t + kKeys > full;
         if (masked) r.hide(x, t);
+        r.raise(r.largest(x), w.scale2);
         r.weights(x, w.scale2, p);
         if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kEach) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");

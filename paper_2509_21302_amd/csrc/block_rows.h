@@ -40,32 +40,36 @@ struct ResidualNorm {
 };
 hipError_t run_residual_norm(const ResidualNorm &a, hipStream_t stream);
 
-// ---- eight consecutive channels of a row
+// ---- eight consecutive channels of a row, as they come from memory
+template <bool F32>
 struct Eight {
-    uint32_t w[8];                  // bf16: half of them
+    uint4 w[F32 ? 2 : 1];
 
-    __device__ void load(const void *row, bool f32, int first)
+    __device__ void load(const void *row, int first)
     {
-        if (f32) {
+        const uint4 *const from = reinterpret_cast<const uint4 *>(static_cast<const char *>(row) + (F32 ? 4 : 2) * first);
+#pragma unroll
+        for (int i = 0; i < (F32 ? 2 : 1); ++i) w[i] = from[i];
+    }
+    __device__ void floats(float (&y)[8]) const
+    {
+        if constexpr (F32) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const uint4 v = reinterpret_cast<const uint4 *>(static_cast<const float *>(row) + first)[i];
-                w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+                y[4 * i] = __uint_as_float(w[i].x); y[4 * i + 1] = __uint_as_float(w[i].y);
+                y[4 * i + 2] = __uint_as_float(w[i].z); y[4 * i + 3] = __uint_as_float(w[i].w);
             }
         } else {
-            const uint4 v = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(row) + first);
-            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+            const uint32_t v[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = __uint_as_float(i & 1 ? v[i / 2] & 0xffff0000u : v[i / 2] << 16);
         }
     }
-    __device__ void floats(bool f32, float (&y)[8]) const
-    {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = f32 ? __uint_as_float(w[i]) : __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
-    }
 };
-__device__ inline void store_eight(void *row, bool f32, int first, const float (&y)[8])
+template <bool F32>
+__device__ inline void store_eight(void *row, int first, const float (&y)[8])
 {
-    if (f32) {
+    if constexpr (F32) {
         float4 *const to = reinterpret_cast<float4 *>(static_cast<float *>(row) + first);
         to[0] = make_float4(y[0], y[1], y[2], y[3]);
         to[1] = make_float4(y[4], y[5], y[6], y[7]);

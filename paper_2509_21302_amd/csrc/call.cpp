@@ -15,6 +15,10 @@
 //   -> the entry point's status, or NotImplemented, before anything is launched, where a call is not an ordinary one (an argument of another type, shape or kind than those
 //      functions take): they refuse it, or take it, then.
 // bind_kv4(which, address): their C entry points, in this order.
+//
+// heads_norm_rope(Q, K, Q_out, K_out, norm, eps, q_gain, q_bias, k_gain, k_bias, rope, positions, rope_pair, pair_axis), attention(Q, K, V, scale, causal, q_starts, kv_starts, kv_lens, max_q,
+// max_kv, out, workspace) and residual_norm(x, y, x_out, h, post_norm, post_gain, post_bias, scale, gate, norm, gain, bias, mod_scale, mod_shift, row_of, eps): the same for the operators around
+// a block's layers; a tensor of another device than the current one is not an ordinary one for these.  bind_block(which, address): their C entry points, in this order.
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -275,6 +279,173 @@ PyObject *kv4_attention(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
+// ---- around a block's layers
+enum { kHeads, kPackedAttention, kResidual, kBlock };
+void *block_entry[kBlock];
+using HeadsFn = int (*)(const void *, const void *, int, int, long long, long long, int, int, int, int, float, const void *, const void *, const void *, const void *, const void *, int, int, int,
+                        const void *, int, const void *, void *, void *, long long, long long, void *);
+using PackedAttentionFn = int (*)(const void *, const void *, const void *, int, int, int, long long, long long, long long, int, int, int, float, int, const void *, const void *, const void *, int, int,
+                          int, void *, void *, size_t, void *);
+using ResidualFn = int (*)(const void *, int, const void *, int, int, int, int, const void *, const void *, const void *, const void *, int, const void *, const void *, const void *, const void *,
+                           int, int, long long, const void *, float, void *, void *, int, void *);
+
+bool norm_of(PyObject *o, int *norm)
+{
+    if (!PyUnicode_Check(o)) return false;
+    *norm = PyUnicode_CompareWithASCIIString(o, "none") == 0 ? 0 : PyUnicode_CompareWithASCIIString(o, "layer") == 0 ? 1 : PyUnicode_CompareWithASCIIString(o, "rms") == 0 ? 2 : -1;
+    return *norm >= 0;
+}
+// whether every argument that is a tensor is on a device
+bool all_on(int device, PyObject *const *args, Py_ssize_t n)
+{
+    for (Py_ssize_t i = 0; i < n; ++i)
+        if (THPVariable_Check(args[i])) {
+            const at::Tensor &t = THPVariable_Unpack(args[i]);
+            if (!t.defined() || !t.is_cuda() || t.get_device() != device) return false;
+        }
+    return true;
+}
+
+PyObject *heads_norm_rope(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        Heads q = {}, k = {}, qo = {}, ko = {};
+        int norm, pair, axes = 0;
+        const void *vec[4], *table = nullptr, *positions = nullptr, *lanes = nullptr;
+        if (n != 14 || block_entry[kHeads] == nullptr || !norm_of(args[4], &norm) || !PyFloat_Check(args[5]) || !whole_number(args[12], &pair)) Py_RETURN_NOTIMPLEMENTED;
+        if (args[0] == Py_None ? args[1] == Py_None : !heads_of(args[0], &q) || !heads_of(args[2], &qo)) Py_RETURN_NOTIMPLEMENTED;
+        if (args[1] != Py_None && (!heads_of(args[1], &k) || !heads_of(args[3], &ko))) Py_RETURN_NOTIMPLEMENTED;
+        const Heads &some = q.t != nullptr ? q : k;
+        auto fits = [&](const Heads &x, const Heads &y) { return x.t == nullptr || (x.T == some.T && x.d == some.d && x.f32 == some.f32 && y.T == x.T && y.heads == x.heads && y.d == x.d && y.f32 == x.f32); };
+        if (!fits(q, qo) || !fits(k, ko)) Py_RETURN_NOTIMPLEMENTED;
+        for (int i = 0; i < 4; ++i)
+            if (!whole_or_none(args[6 + i], at::kFloat, some.d, &vec[i])) Py_RETURN_NOTIMPLEMENTED;
+        int rows = 0, dim = 0;
+        if (args[10] != Py_None) {
+            const at::Tensor *r = ordinary(args[10]), *p = ordinary(args[11]);
+            if (r == nullptr || p == nullptr || r->dim() != 2 || r->scalar_type() != at::kFloat || r->size(0) > INT32_MAX || r->size(1) > INT32_MAX || p->scalar_type() != at::kInt) Py_RETURN_NOTIMPLEMENTED;
+            axes = p->dim() == 2 && p->size(0) <= 4 ? (int)p->size(0) : p->dim() == 1 ? 1 : 0;
+            if (axes == 0 || p->numel() != (long long)axes * some.T) Py_RETURN_NOTIMPLEMENTED;
+            table = r->const_data_ptr();
+            rows = (int)r->size(0);
+            dim = (int)r->size(1);
+            positions = p->const_data_ptr();
+            if (!whole_or_none(args[13], at::kByte, dim / 2, &lanes)) Py_RETURN_NOTIMPLEMENTED;
+        }
+        if (!all_on(c10::hip::current_device(), args, n)) Py_RETURN_NOTIMPLEMENTED;
+        auto at = [](const Heads &h) { return h.t != nullptr ? h.t->data_ptr() : nullptr; };
+        const void *qp = at(q), *kp = at(k);
+        void *qop = at(qo), *kop = at(ko), *stream = current_stream();
+        const float eps = (float)PyFloat_AS_DOUBLE(args[5]);
+        int status;
+        Py_BEGIN_ALLOW_THREADS
+        status = reinterpret_cast<HeadsFn>(block_entry[kHeads])(qp, kp, some.f32, some.T, q.stride, k.stride, q.heads, k.heads, some.d, norm, eps, vec[0], vec[1], vec[2], vec[3], table, rows, dim, pair,
+                                                               positions, axes, lanes, qop, kop, qo.stride, ko.stride, stream);
+        Py_END_ALLOW_THREADS
+        return PyLong_FromLong(status);
+    });
+}
+
+PyObject *attention(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        Heads q, k, v, out;
+        int causal, max_q, max_kv;
+        if (n != 12 || block_entry[kPackedAttention] == nullptr || !heads_of(args[0], &q) || !heads_of(args[1], &k) || !heads_of(args[2], &v) || !heads_of(args[10], &out) || q.f32 || k.f32 || v.f32 ||
+            out.f32 || k.T != v.T || k.heads != v.heads || k.d != q.d || v.d != q.d || !out.t->is_contiguous() || out.T != q.T || out.heads != q.heads || out.d != q.d || !PyFloat_Check(args[3]) ||
+            !whole_number(args[4], &causal) || !whole_number(args[8], &max_q) || !whole_number(args[9], &max_kv))
+            Py_RETURN_NOTIMPLEMENTED;
+        const at::Tensor *starts = ordinary(args[5]), *ws = nullptr;
+        const void *kv_starts, *lens;
+        if (starts == nullptr || starts->scalar_type() != at::kInt || starts->numel() < 1 || starts->numel() > INT32_MAX) Py_RETURN_NOTIMPLEMENTED;
+        const long long seqs = starts->numel() - 1;
+        if (!whole(args[6], at::kInt, seqs + (args[7] == Py_None), &kv_starts) || !whole_or_none(args[7], at::kInt, seqs, &lens)) Py_RETURN_NOTIMPLEMENTED;
+        if ((args[11] != Py_None && (ws = ordinary(args[11])) == nullptr) || !all_on(c10::hip::current_device(), args, n)) Py_RETURN_NOTIMPLEMENTED;
+        const void *qp = q.t->const_data_ptr(), *kp = k.t->const_data_ptr(), *vp = v.t->const_data_ptr(), *sp = starts->const_data_ptr();
+        void *op = out.t->data_ptr(), *wp = ws != nullptr ? ws->data_ptr() : nullptr, *stream = current_stream();
+        const size_t bytes = ws != nullptr ? (size_t)ws->numel() * ws->element_size() : 0;
+        const float scale = (float)PyFloat_AS_DOUBLE(args[3]);
+        int status;
+        Py_BEGIN_ALLOW_THREADS
+        status = reinterpret_cast<PackedAttentionFn>(block_entry[kPackedAttention])(qp, kp, vp, 0, q.T, k.T, q.stride, k.stride, v.stride, q.heads, k.heads, q.d, scale, causal, sp, kv_starts, lens, (int)seqs, max_q,
+                                                                   max_kv, op, wp, bytes, stream);
+        Py_END_ALLOW_THREADS
+        return PyLong_FromLong(status);
+    });
+}
+
+PyObject *residual_norm(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        int post_norm, norm, rows = 0, dtype = 0;
+        long long stride = 0;
+        const at::Tensor *const x = n == 16 ? ordinary(args[0]) : nullptr;
+        if (x == nullptr || block_entry[kResidual] == nullptr || x->dim() != 2 || x->size(0) > INT32_MAX || x->size(1) > INT32_MAX || !norm_of(args[4], &post_norm) || !norm_of(args[9], &norm) ||
+            !PyFloat_Check(args[15]))
+            Py_RETURN_NOTIMPLEMENTED;
+        const int M = (int)x->size(0), C = (int)x->size(1);
+        auto type_of = [](const at::Tensor *t) { return t->scalar_type() == at::kBFloat16 ? 0 : t->scalar_type() == at::kFloat ? 1 : -1; };
+        const int x_type = type_of(x);
+        const at::Tensor *other[3] = {nullptr, nullptr, nullptr};      // y, x_out, h
+        int types[3] = {0, x_type, 0};
+        for (int i = 0; i < 3; ++i)
+            if (args[1 + i] != Py_None) {
+                other[i] = ordinary(args[1 + i]);
+                if (other[i] == nullptr || other[i]->dim() != 2 || other[i]->size(0) != M || other[i]->size(1) != C || (types[i] = type_of(other[i])) < 0) Py_RETURN_NOTIMPLEMENTED;
+            }
+        if (x_type < 0 || types[1] != x_type) Py_RETURN_NOTIMPLEMENTED;
+        const void *vec[5], *cond[3] = {nullptr, nullptr, nullptr}, *row_of;
+        const int vec_at[5] = {5, 6, 7, 10, 11}, cond_at[3] = {8, 12, 13};
+        for (int i = 0; i < 5; ++i)
+            if (!whole_or_none(args[vec_at[i]], at::kFloat, C, &vec[i])) Py_RETURN_NOTIMPLEMENTED;
+        bool any = false;
+        for (int i = 0; i < 3; ++i) {
+            PyObject *const o = args[cond_at[i]];
+            if (o == Py_None) continue;
+            if (!THPVariable_CheckExact(o)) Py_RETURN_NOTIMPLEMENTED;
+            const at::Tensor &t = THPVariable_Unpack(o);
+            if (!t.defined() || t.layout() != at::kStrided || !t.has_storage() || !t.is_cuda() || t.is_conj() || t.is_neg() || t.dim() != 2 || t.size(0) < 1 || t.size(0) > INT32_MAX || t.size(1) != C ||
+                t.stride(1) != 1)
+                Py_RETURN_NOTIMPLEMENTED;
+            const int type = type_of(&t);
+            const long long apart = t.size(0) > 1 ? (long long)t.stride(0) : C;
+            if (type < 0 || (any && (t.size(0) != rows || type != dtype || apart != stride))) Py_RETURN_NOTIMPLEMENTED;
+            any = true;
+            rows = (int)t.size(0);
+            dtype = type;
+            stride = apart;
+            cond[i] = t.const_data_ptr();
+        }
+        if (!whole_or_none(args[14], at::kInt, M, &row_of) || !all_on(c10::hip::current_device(), args, n)) Py_RETURN_NOTIMPLEMENTED;
+        const void *xp = x->const_data_ptr(), *yp = other[0] != nullptr ? other[0]->const_data_ptr() : nullptr;
+        void *xo = other[1] != nullptr ? other[1]->data_ptr() : nullptr, *hp = other[2] != nullptr ? other[2]->data_ptr() : nullptr, *stream = current_stream();
+        const float eps = (float)PyFloat_AS_DOUBLE(args[15]);
+        int status;
+        Py_BEGIN_ALLOW_THREADS
+        status = reinterpret_cast<ResidualFn>(block_entry[kResidual])(xp, x_type, yp, types[0], M, C, post_norm, vec[0], vec[1], vec[2], cond[0], norm, vec[3], vec[4], cond[1], cond[2], dtype, rows,
+                                                                     stride, row_of, eps, xo, hp, types[2], stream);
+        Py_END_ALLOW_THREADS
+        return PyLong_FromLong(status);
+    });
+}
+
+PyObject *bind_block(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 2) {
+        PyErr_SetString(PyExc_TypeError, "bind_block takes 2 arguments");
+        return nullptr;
+    }
+    const long which = PyLong_AsLong(args[0]);
+    void *const address = PyLong_AsVoidPtr(args[1]);
+    if (PyErr_Occurred()) return nullptr;
+    if (which < 0 || which >= kBlock) {
+        PyErr_SetString(PyExc_ValueError, "no such entry point");
+        return nullptr;
+    }
+    block_entry[which] = address;
+    Py_RETURN_NONE;
+}
+
 PyObject *bind_kv4(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     if (n != 2) {
@@ -312,7 +483,8 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n)
 using Fast = PyObject *(*)(PyObject *, PyObject *const *, Py_ssize_t);
 PyMethodDef method(const char *name, Fast f) { return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}; }
 PyMethodDef methods[] = {method("linear", linear), method("bind", bind), method("kv4_append", kv4_append), method("kv4_read", kv4_read), method("kv4_attention", kv4_attention),
-                         method("bind_kv4", bind_kv4),
+                         method("bind_kv4", bind_kv4), method("heads_norm_rope", heads_norm_rope), method("attention", attention), method("residual_norm", residual_norm),
+                         method("bind_block", bind_block),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

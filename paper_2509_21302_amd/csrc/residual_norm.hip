@@ -56,7 +56,19 @@ __device__ inline void normalise(float (&y)[V][8], int kind, int C, float eps, i
         for (int i = 0; i < 8; ++i) y[v][i] *= f;
 }
 
-template <int LANES, int V>
+// Eight channels of a condition's row.
+__device__ inline void load_cond(const void *row, bool f32, int first, float (&u)[8])
+{
+    if (f32) {
+        load_eight(static_cast<const float *>(row) + first, u);
+    } else {
+        Eight<false> raw;
+        raw.load(row, first);
+        raw.floats(u);
+    }
+}
+
+template <int LANES, int V, bool XF, bool YF, bool HF>
 __global__ __launch_bounds__(256) void residual_norm_kernel(ResidualNorm a)
 {
     __shared__ float red[4];
@@ -64,15 +76,16 @@ __global__ __launch_bounds__(256) void residual_norm_kernel(ResidualNorm a)
     const long long row = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
     if (row >= a.M) return;
     const size_t at = (size_t)row * a.C;
-    const char *const x_row = static_cast<const char *>(a.x) + at * (a.x_f32 ? 4 : 2), *const y_row = static_cast<const char *>(a.y) + at * (a.y_f32 ? 4 : 2);
+    const char *const x_row = static_cast<const char *>(a.x) + at * (XF ? 4 : 2), *const y_row = static_cast<const char *>(a.y) + at * (YF ? 4 : 2);
     auto piece = [&](int v) { return (v * LANES + lane) * 8; };
     auto there = [&](int v) { return piece(v) < a.C; };
-    Eight raw_x[V], raw_y[V];
+    Eight<XF> raw_x[V];
+    Eight<YF> raw_y[V];
 #pragma unroll
     for (int v = 0; v < V; ++v)
         if (there(v)) {
-            raw_x[v].load(x_row, a.x_f32, piece(v));
-            if (a.y != nullptr) raw_y[v].load(y_row, a.y_f32, piece(v));
+            raw_x[v].load(x_row, piece(v));
+            if (a.y != nullptr) raw_y[v].load(y_row, piece(v));
         }
     const bool conditioned = a.gate != nullptr || a.mod_scale != nullptr || a.mod_shift != nullptr;
     const int r = !conditioned ? 0 : a.row_of != nullptr ? min(max(a.row_of[row], 0), a.cond_rows - 1) : a.cond_rows == 1 ? 0 : (int)row;
@@ -82,7 +95,7 @@ __global__ __launch_bounds__(256) void residual_norm_kernel(ResidualNorm a)
     if (a.y != nullptr) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            raw_y[v].floats(a.y_f32, x[v]);
+            raw_y[v].floats(x[v]);
             if (!there(v))
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[v][i] = 0.0f;
@@ -108,9 +121,7 @@ __global__ __launch_bounds__(256) void residual_norm_kernel(ResidualNorm a)
                     for (int i = 0; i < 8; ++i) x[v][i] *= u[i];
                 }
                 if (a.gate != nullptr) {
-                    Eight raw;
-                    raw.load(static_cast<const char *>(a.gate) + cond, a.cond_f32, piece(v));
-                    raw.floats(a.cond_f32, u);
+                    load_cond(static_cast<const char *>(a.gate) + cond, a.cond_f32, piece(v), u);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) x[v][i] *= u[i];
                 }
@@ -119,10 +130,10 @@ __global__ __launch_bounds__(256) void residual_norm_kernel(ResidualNorm a)
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         float u[8];
-        raw_x[v].floats(a.x_f32, u);
+        raw_x[v].floats(u);
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[v][i] = !there(v) ? 0.0f : a.y != nullptr ? u[i] + x[v][i] : u[i];
-        if (a.x_out != nullptr && there(v)) store_eight(static_cast<char *>(a.x_out) + at * (a.x_f32 ? 4 : 2), a.x_f32, piece(v), x[v]);
+        if (a.x_out != nullptr && there(v)) store_eight<XF>(static_cast<char *>(a.x_out) + at * (XF ? 4 : 2), piece(v), x[v]);
     }
     if (a.h == nullptr) return;
     normalise<LANES, V>(x, a.norm, a.C, a.eps, lane, red);
@@ -130,7 +141,6 @@ __global__ __launch_bounds__(256) void residual_norm_kernel(ResidualNorm a)
     for (int v = 0; v < V; ++v)
         if (there(v)) {
             float u[8];
-            Eight raw;
             if (a.gain != nullptr) {
                 load_eight(a.gain + piece(v), u);
 #pragma unroll
@@ -142,39 +152,51 @@ __global__ __launch_bounds__(256) void residual_norm_kernel(ResidualNorm a)
                 for (int i = 0; i < 8; ++i) x[v][i] += u[i];
             }
             if (a.mod_scale != nullptr) {
-                raw.load(static_cast<const char *>(a.mod_scale) + cond, a.cond_f32, piece(v));
-                raw.floats(a.cond_f32, u);
+                load_cond(static_cast<const char *>(a.mod_scale) + cond, a.cond_f32, piece(v), u);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[v][i] = fmaf(x[v][i], u[i], x[v][i]);
             }
             if (a.mod_shift != nullptr) {
-                raw.load(static_cast<const char *>(a.mod_shift) + cond, a.cond_f32, piece(v));
-                raw.floats(a.cond_f32, u);
+                load_cond(static_cast<const char *>(a.mod_shift) + cond, a.cond_f32, piece(v), u);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[v][i] += u[i];
             }
-            store_eight(static_cast<char *>(a.h) + at * (a.h_f32 ? 4 : 2), a.h_f32, piece(v), x[v]);
+            store_eight<HF>(static_cast<char *>(a.h) + at * (HF ? 4 : 2), piece(v), x[v]);
         }
 }
 
-template <int LANES, int V>
+template <int LANES, int V, bool XF, bool YF, bool HF>
 hipError_t launch(const ResidualNorm &a, hipStream_t stream)
 {
-    residual_norm_kernel<LANES, V><<<dim3((unsigned)(((long long)a.M * LANES + 255) / 256)), 256, 0, stream>>>(a);
+    residual_norm_kernel<LANES, V, XF, YF, HF><<<dim3((unsigned)(((long long)a.M * LANES + 255) / 256)), 256, 0, stream>>>(a);
     return hipGetLastError();
+}
+template <bool XF, bool YF, bool HF>
+hipError_t launch(const ResidualNorm &a, hipStream_t stream)
+{
+    if (a.C <= 128) return launch<16, 1, XF, YF, HF>(a, stream);
+    if (a.C <= 256) return launch<16, 2, XF, YF, HF>(a, stream);
+    if (a.C <= 512) return launch<64, 1, XF, YF, HF>(a, stream);
+    if (a.C <= 1024) return launch<64, 2, XF, YF, HF>(a, stream);
+    if (a.C <= 2048) return launch<64, 4, XF, YF, HF>(a, stream);
+    if (a.C <= 4096) return launch<256, 2, XF, YF, HF>(a, stream);
+    return launch<256, 4, XF, YF, HF>(a, stream);
 }
 
 }  // namespace
 
 hipError_t run_residual_norm(const ResidualNorm &a, hipStream_t stream)
 {
-    if (a.C <= 128) return launch<16, 1>(a, stream);
-    if (a.C <= 256) return launch<16, 2>(a, stream);
-    if (a.C <= 512) return launch<64, 1>(a, stream);
-    if (a.C <= 1024) return launch<64, 2>(a, stream);
-    if (a.C <= 2048) return launch<64, 4>(a, stream);
-    if (a.C <= 4096) return launch<256, 2>(a, stream);
-    return launch<256, 4>(a, stream);
+    switch (a.x_f32 * 4 + a.y_f32 * 2 + a.h_f32) {
+        case 0: return launch<false, false, false>(a, stream);
+        case 1: return launch<false, false, true>(a, stream);
+        case 2: return launch<false, true, false>(a, stream);
+        case 3: return launch<false, true, true>(a, stream);
+        case 4: return launch<true, false, false>(a, stream);
+        case 5: return launch<true, false, true>(a, stream);
+        case 6: return launch<true, true, false>(a, stream);
+        default: return launch<true, true, true>(a, stream);
+    }
 }
 
 }  // namespace qvggt
