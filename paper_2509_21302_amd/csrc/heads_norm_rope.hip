@@ -1,7 +1,9 @@
 // Heads of queries and keys, as they lie in the rows of a fused product: norm over a head's channels, gain and bias, rotation by positions with several axes.
 //
-// d / 8 lanes have a head, eight channels each, and a wave has heads of one token: what turns them (the token's positions, its rows of the table) is loaded once for all of its heads.  Means and
-// variances are two passes over registers, sums between lanes by DPP, and so are the channels that a lane's own turn with.
+// d / 8 lanes have a head, eight channels each, and a wave has heads of one token: what turns them (the token's positions, its rows of the table) is found once for all of them, one pair of channels
+// a lane, and handed out through LDS (16411 tokens of 32 + 8 heads x 128 in float32, three axes whose pairs take turns: 134 us; 164 with every lane finding all of its own).  Means and variances are two
+// passes over registers, sums between lanes by DPP, and so are the channels that a lane's own turn with.  Bound by memory: 5.0 TB/s there, 5.3 on ten frames (13740 tokens of 16 + 16 heads x 64 in
+// bf16: 21 us), read and written, where a copy reaches 4.8 to 5.0.
 #include "block_rows.h"
 
 namespace qvggt {
@@ -16,109 +18,127 @@ __device__ inline float sum_over(float v)
     return LANES == 8 ? v : dpp_add_step<0x140>(v);
 }
 
-// HEADS: of a lane, whose loads are in flight together.  Chunks of a token: of queries first, of keys then.
+// HEADS: of a lane, whose loads are in flight together: a chunk.  A token's chunks are those of its queries, then those of its keys; a wave has `each` of them.
 template <int D, bool F32, int HEADS>
-__global__ __launch_bounds__(256) void heads_norm_rope_kernel(HeadsNormRope a, int chunks_q, int chunks)
+__global__ __launch_bounds__(256) void heads_norm_rope_kernel(HeadsNormRope a, int chunks_q, int chunks, int each)
 {
     constexpr int kLanes = D / 8, kGroups = 64 / kLanes, kSize = F32 ? 4 : 2;
-    const int lane = threadIdx.x & 63, id = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int token = id / chunks, chunk = id % chunks;
+    __shared__ __align__(16) float angles[4][2][D / 2];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = (chunks + each - 1) / each;
+    const int id = blockIdx.x * 4 + wave, token = id / waves, chunk0 = id % waves * each, stop = min(chunk0 + each, chunks);
     if (token >= a.T) return;
-    const bool of_keys = chunk >= chunks_q;
-    const int first = (lane % kLanes) * 8, heads = of_keys ? a.heads[1] : a.heads[0], head0 = (of_keys ? chunk - chunks_q : chunk) * HEADS * kGroups + lane / kLanes;
-    const char *const in = static_cast<const char *>(of_keys ? a.in[1] : a.in[0]) + kSize * token * (of_keys ? a.in_stride[1] : a.in_stride[0]);
-    char *const out = static_cast<char *>(of_keys ? a.out[1] : a.out[0]) + kSize * token * (of_keys ? a.out_stride[1] : a.out_stride[0]);
-    const float *const g = of_keys ? a.gain[1] : a.gain[0], *const b = of_keys ? a.bias[1] : a.bias[0];
-    Eight<F32> raw[HEADS];
+    const int first = (lane % kLanes) * 8, group = lane / kLanes;
+    struct Place {
+        bool of_keys;
+        int head0, heads;
+    };
+    auto place = [&](int chunk) {
+        const bool of_keys = chunk >= chunks_q;
+        return Place{of_keys, (of_keys ? chunk - chunks_q : chunk) * HEADS * kGroups + group, of_keys ? a.heads[1] : a.heads[0]};
+    };
+    Eight<F32> next[HEADS];
+    auto load = [&](int chunk) {
+        const Place p = place(chunk);
+        const char *const in = static_cast<const char *>(p.of_keys ? a.in[1] : a.in[0]) + kSize * token * (p.of_keys ? a.in_stride[1] : a.in_stride[0]);
 #pragma unroll
-    for (int k = 0; k < HEADS; ++k) raw[k].load(in + (size_t)kSize * D * min(head0 + k * kGroups, heads - 1), first);
-    float gain[8], bias[8];
-    if (g != nullptr) load_eight(g + first, gain);
-    if (b != nullptr) load_eight(b + first, bias);
+        for (int k = 0; k < HEADS; ++k) next[k].load(in + (size_t)kSize * D * min(p.head0 + k * kGroups, p.heads - 1), first);
+    };
+    load(chunk0);
 
-    // The angles of this lane's channels: eight cosines and sines, or four where channels turn with others of the lane
+    // A lane finds the angle of one pair of channels; through LDS, where every lane then has those of its channels: eight cosines and sines, or four where channels turn with others of the lane
     const bool turns = a.rope != nullptr && first < a.dim, wide = a.pair >= 8;
     float cosine[8], sine[8];
     if (a.rope != nullptr) {
-        const int c = turns ? first : 0, half = a.dim / 2;
+        const int half = a.dim / 2;
+        if (lane < half) {
+            const int section = lane * a.axes;
+            const int axis = min(a.pair_axis != nullptr ? a.pair_axis[lane] : (section >= half) + (section >= 2 * half) + (section >= 3 * half), a.axes - 1);
+            const float *const angle = a.rope + (size_t)min(max(a.positions[(size_t)axis * a.T + token], 0), a.rows - 1) * a.dim + lane;
+            angles[wave][0][lane] = angle[0];
+            angles[wave][1][lane] = angle[half];
+        }
+        lanes_exchange_fence();
+        const int c = turns ? first : 0;
         const int p0 = wide ? c / (2 * a.pair) * a.pair + (c & (a.pair - 1)) : c / 2;
-        int at[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) at[i] = i < a.axes ? min(max(a.positions[(size_t)i * a.T + token], 0), a.rows - 1) : 0;
-        auto axis_of = [&](int p) {
-            const int section = p * a.axes;
-            return min(a.pair_axis != nullptr ? a.pair_axis[p] : (section >= half) + (section >= 2 * half) + (section >= 3 * half), a.axes - 1);
-        };
-        auto row_of = [&](int axis) { return axis == 0 ? at[0] : axis == 1 ? at[1] : axis == 2 ? at[2] : at[3]; };
-        if (wide && (a.axes == 1 || (a.pair_axis == nullptr && half % (8 * a.axes) == 0))) {        // the angles of one row
-            const float *const angle = a.rope + (size_t)row_of(a.axes == 1 ? 0 : axis_of(p0)) * a.dim + p0;
-            load_eight(angle, cosine);
-            load_eight(angle + half, sine);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (i >= 4 && !wide) break;
-                const float *const angle = a.rope + (size_t)row_of(axis_of(p0 + i)) * a.dim + p0 + i;
-                cosine[i] = angle[0];
-                sine[i] = angle[half];
-            }
+        for (int i = 0; i < 8; i += 4) {
+            const int p = p0 + (wide ? i : 0);              // (the second four are nobody's where pairs are inside a lane)
+            const float4 u = *reinterpret_cast<const float4 *>(&angles[wave][0][p]), v = *reinterpret_cast<const float4 *>(&angles[wave][1][p]);
+            cosine[i] = u.x; cosine[i + 1] = u.y; cosine[i + 2] = u.z; cosine[i + 3] = u.w;
+            sine[i] = v.x; sine[i + 1] = v.y; sine[i + 2] = v.z; sine[i + 3] = v.w;
         }
     }
+    float gain[8], bias[8];
+    const float *g = nullptr, *b = nullptr;
+    for (int chunk = chunk0; chunk < stop; ++chunk) {
+        const Place here = place(chunk);
+        char *const out = static_cast<char *>(here.of_keys ? a.out[1] : a.out[0]) + kSize * token * (here.of_keys ? a.out_stride[1] : a.out_stride[0]);
+        if (chunk == chunk0 || chunk == chunks_q) {
+            g = here.of_keys ? a.gain[1] : a.gain[0];
+            b = here.of_keys ? a.bias[1] : a.bias[0];
+            if (g != nullptr) load_eight(g + first, gain);
+            if (b != nullptr) load_eight(b + first, bias);
+        }
+        Eight<F32> raw[HEADS];
 #pragma unroll
-    for (int k = 0; k < HEADS; ++k) {
-        float y[8];
-        raw[k].floats(y);
-        if (a.norm != kNormNone) {
-            if (a.norm == kNormLayer) {
+        for (int k = 0; k < HEADS; ++k) raw[k] = next[k];
+        if (chunk + 1 < stop) load(chunk + 1);
+#pragma unroll
+        for (int k = 0; k < HEADS; ++k) {
+            float y[8];
+            raw[k].floats(y);
+            if (a.norm != kNormNone) {
+                if (a.norm == kNormLayer) {
+                    float s = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s += y[i];
+                    const float mean = sum_over<kLanes>(s) * (1.0f / D);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) y[i] -= mean;
+                }
                 float s = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) s += y[i];
-                const float mean = sum_over<kLanes>(s) * (1.0f / D);
+                for (int i = 0; i < 8; ++i) s = fmaf(y[i], y[i], s);
+                const float f = inverse_root(sum_over<kLanes>(s) * (1.0f / D) + a.eps);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] -= mean;
+                for (int i = 0; i < 8; ++i) y[i] *= f;
             }
-            float s = 0.0f;
+            if (g != nullptr)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s = fmaf(y[i], y[i], s);
-            const float f = inverse_root(sum_over<kLanes>(s) * (1.0f / D) + a.eps);
+                for (int i = 0; i < 8; ++i) y[i] *= gain[i];
+            if (b != nullptr)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] *= f;
-        }
-        if (g != nullptr)
+                for (int i = 0; i < 8; ++i) y[i] += bias[i];
+            if (a.rope != nullptr) {
+                float z[8];
+                auto across = [&](auto other) {
+                    const float side = first & a.pair ? 1.0f : -1.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] *= gain[i];
-        if (b != nullptr)
+                    for (int i = 0; i < 8; ++i) z[i] = fmaf(y[i], cosine[i], side * sine[i] * other(y[i]));
+                };
+                auto within = [&](auto pair) {
+                    constexpr int kPair = decltype(pair)::value;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] += bias[i];
-        if (a.rope != nullptr) {
-            float z[8];
-            auto across = [&](auto other) {
-                const float side = first & a.pair ? 1.0f : -1.0f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) z[i] = fmaf(y[i], cosine[i], side * sine[i] * other(y[i]));
-            };
-            auto within = [&](auto pair) {
-                constexpr int kPair = decltype(pair)::value;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    constexpr int kAll = 2 * kPair;
-                    const int angle = i / kAll * kPair + i % kPair;
-                    z[i] = fmaf(y[i], cosine[angle], (i & kPair ? sine[angle] : -sine[angle]) * y[i ^ kPair]);
+                    for (int i = 0; i < 8; ++i) {
+                        constexpr int kAll = 2 * kPair;
+                        const int angle = i / kAll * kPair + i % kPair;
+                        z[i] = fmaf(y[i], cosine[angle], (i & kPair ? sine[angle] : -sine[angle]) * y[i ^ kPair]);
+                    }
+                };
+                switch (a.pair) {
+                    case 1: within(std::integral_constant<int, 1>()); break;
+                    case 2: within(std::integral_constant<int, 2>()); break;
+                    case 4: within(std::integral_constant<int, 4>()); break;
+                    case 8: across([](float v) { return dpp_move<0xB1>(v); }); break;
+                    case 16: across([](float v) { return dpp_move<0x4E>(v); }); break;
+                    case 32: across([](float v) { return dpp_move<0x141>(dpp_move<0x1B>(v)); }); break;
+                    default: across([](float v) { return dpp_move<0x128>(v); }); break;
                 }
-            };
-            switch (a.pair) {
-                case 1: within(std::integral_constant<int, 1>()); break;
-                case 2: within(std::integral_constant<int, 2>()); break;
-                case 4: within(std::integral_constant<int, 4>()); break;
-                case 8: across([](float v) { return dpp_move<0xB1>(v); }); break;
-                case 16: across([](float v) { return dpp_move<0x4E>(v); }); break;
-                case 32: across([](float v) { return dpp_move<0x141>(dpp_move<0x1B>(v)); }); break;
-                default: across([](float v) { return dpp_move<0x128>(v); }); break;
-            }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = turns ? z[i] : y[i];
+                for (int i = 0; i < 8; ++i) y[i] = turns ? z[i] : y[i];
+            }
+            if (here.head0 + k * kGroups < here.heads) store_eight<F32>(out + (size_t)kSize * D * (here.head0 + k * kGroups), first, y);
         }
-        if (head0 + k * kGroups < heads) store_eight<F32>(out + (size_t)kSize * D * (head0 + k * kGroups), first, y);
     }
 }
 
@@ -127,7 +147,9 @@ hipError_t launch(const HeadsNormRope &a, hipStream_t stream)
 {
     constexpr int kGroups = 64 / (D / 8);
     const int chunks_q = (a.heads[0] + HEADS * kGroups - 1) / (HEADS * kGroups), chunks = chunks_q + (a.heads[1] + HEADS * kGroups - 1) / (HEADS * kGroups);
-    heads_norm_rope_kernel<D, F32, HEADS><<<dim3((unsigned)(((long long)a.T * chunks + 3) / 4)), 256, 0, stream>>>(a, chunks_q, chunks);
+    // all of a token's chunks where there are tokens enough for all waves of the chip (13740 tokens of 16 + 16 heads x 64 in bf16: 28 us for 31)
+    const int each = a.T >= 2048 ? chunks : 1, waves = (chunks + each - 1) / each;
+    heads_norm_rope_kernel<D, F32, HEADS><<<dim3((unsigned)(((long long)a.T * waves + 3) / 4)), 256, 0, stream>>>(a, chunks_q, chunks, each);
     return hipGetLastError();
 }
 // Four heads a lane, or fewer where there are no more

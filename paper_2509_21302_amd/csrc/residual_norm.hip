@@ -1,7 +1,9 @@
 // What a block's output does to the residual stream, and the norm in front of the next block:
 //     x' = x + scale gate[r] norm_post(y),      h = norm_pre(x') (1 + mod_scale[r]) + mod_shift[r].
 //
-// One pass: LANES lanes have a row, every one V pieces of eight channels, in registers from the first load to the last store; means and variances are two passes over registers.
+// One pass: LANES lanes have a row, every one V pieces of eight channels, in registers from the first load to the last store; means and variances are two passes over registers.  Bound by memory:
+// 5.4 to 5.9 TB/s, read and written, from 128 to 8192 channels (137400 rows of 1024 in bf16: 192 us), where a copy reaches 4.8 to 5.0; 4.5 with gains, gate, scale and shift of everything, which are
+// more bytes a row than the row itself, out of L2.
 #include "block_rows.h"
 
 namespace qvggt {
@@ -20,7 +22,8 @@ __device__ inline float row_sum(float v, float *red)
     if (LANES == 64) return v;
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
-    v = (red[0] + red[1]) + (red[2] + red[3]);
+    v = 0.0f;
+    for (int i = 0; i < (int)blockDim.x / 64; ++i) v += red[i];
     __syncthreads();
     return v;
 }
@@ -46,7 +49,7 @@ __device__ inline void normalise(float (&y)[V][8], int kind, int C, float eps, i
     float s = 0.0f;
 #pragma unroll
     for (int v = 0; v < V; ++v)
-        if ((v * LANES + lane) * 8 < C)
+        if ((v * (LANES ? LANES : 64) + lane) * 8 < C)
 #pragma unroll
             for (int i = 0; i < 8; ++i) s = fmaf(y[v][i], y[v][i], s);
     const float f = inverse_root(row_sum<LANES>(s, red) * share + eps);
@@ -56,28 +59,48 @@ __device__ inline void normalise(float (&y)[V][8], int kind, int C, float eps, i
         for (int i = 0; i < 8; ++i) y[v][i] *= f;
 }
 
-// Eight channels of a condition's row.
-__device__ inline void load_cond(const void *row, bool f32, int first, float (&u)[8])
+// Eight channels of a row of a condition, or of a vector; what is not given is not looked at.
+__device__ inline void load_cond(const void *rows, size_t at, bool f32, int first, float (&u)[8])
 {
+    if (rows == nullptr) return;
+    const char *const row = static_cast<const char *>(rows) + at;
     if (f32) {
-        load_eight(static_cast<const float *>(row) + first, u);
+        load_eight(reinterpret_cast<const float *>(row) + first, u);
     } else {
         Eight<false> raw;
         raw.load(row, first);
         raw.floats(u);
     }
 }
-
-template <int LANES, int V, bool XF, bool YF, bool HF>
-__global__ __launch_bounds__(256) void residual_norm_kernel(ResidualNorm a)
+__device__ inline void load_given(const float *from, int first, float (&u)[8])
 {
-    __shared__ float red[4];
-    const int lane = threadIdx.x % LANES;
-    const long long row = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    if (from != nullptr) load_eight(from + first, u);
+}
+__device__ inline void multiply(const void *given, float (&x)[8], const float (&u)[8])
+{
+    if (given != nullptr)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= u[i];
+}
+__device__ inline void add(const void *given, float (&x)[8], const float (&u)[8])
+{
+    if (given != nullptr)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] += u[i];
+}
+
+// LANES = 0: a block has a row, of as many lanes as it has pieces.
+template <int LANES, int V, bool XF, bool YF, bool HF>
+__global__ __launch_bounds__(LANES ? 256 : 1024) void residual_norm_kernel(ResidualNorm a)
+{
+    constexpr int kLanes = LANES ? LANES : 64;          // (LANES = 0 has V = 1)
+    __shared__ float red[16];
+    const int lane = LANES ? threadIdx.x % kLanes : threadIdx.x;
+    const long long row = LANES ? (long long)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes : blockIdx.x;
     if (row >= a.M) return;
     const size_t at = (size_t)row * a.C;
     const char *const x_row = static_cast<const char *>(a.x) + at * (XF ? 4 : 2), *const y_row = static_cast<const char *>(a.y) + at * (YF ? 4 : 2);
-    auto piece = [&](int v) { return (v * LANES + lane) * 8; };
+    auto piece = [&](int v) { return (v * kLanes + lane) * 8; };
     auto there = [&](int v) { return piece(v) < a.C; };
     Eight<XF> raw_x[V];
     Eight<YF> raw_y[V];
@@ -90,6 +113,26 @@ __global__ __launch_bounds__(256) void residual_norm_kernel(ResidualNorm a)
     const bool conditioned = a.gate != nullptr || a.mod_scale != nullptr || a.mod_shift != nullptr;
     const int r = !conditioned ? 0 : a.row_of != nullptr ? min(max(a.row_of[row], 0), a.cond_rows - 1) : a.cond_rows == 1 ? 0 : (int)row;
     const size_t cond = (size_t)r * a.cond_stride * (a.cond_f32 ? 4 : 2);
+    // What a piece is multiplied by is loaded ahead of the sums where a lane has one piece of a wave's row (400000 rows of 128 channels: 69 us for 74).  Not where a block has the row: the registers
+    // cost more waves than that gains (8191 rows of 2560 with everything given: 66 us for 56; 10000 of 8192: 166 for 124).
+    constexpr bool kAhead = V == 1 && LANES != 0;
+    float post_gain[8], post_bias[8], scale[8], gate[8], gain[8], bias[8], mod_scale[8], mod_shift[8];
+    auto load_post = [&](int v) {
+        load_given(a.post_gain, piece(v), post_gain);
+        load_given(a.post_bias, piece(v), post_bias);
+        load_given(a.scale, piece(v), scale);
+        load_cond(a.gate, cond, a.cond_f32, piece(v), gate);
+    };
+    auto load_pre = [&](int v) {
+        load_given(a.gain, piece(v), gain);
+        load_given(a.bias, piece(v), bias);
+        load_cond(a.mod_scale, cond, a.cond_f32, piece(v), mod_scale);
+        load_cond(a.mod_shift, cond, a.cond_f32, piece(v), mod_shift);
+    };
+    if (kAhead && there(0)) {
+        if (a.y != nullptr) load_post(0);
+        if (a.h != nullptr) load_pre(0);
+    }
 
     float x[V][8];
     if (a.y != nullptr) {
@@ -104,27 +147,11 @@ __global__ __launch_bounds__(256) void residual_norm_kernel(ResidualNorm a)
 #pragma unroll
         for (int v = 0; v < V; ++v)
             if (there(v)) {
-                float u[8];
-                if (a.post_gain != nullptr) {
-                    load_eight(a.post_gain + piece(v), u);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[v][i] *= u[i];
-                }
-                if (a.post_bias != nullptr) {
-                    load_eight(a.post_bias + piece(v), u);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[v][i] += u[i];
-                }
-                if (a.scale != nullptr) {
-                    load_eight(a.scale + piece(v), u);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[v][i] *= u[i];
-                }
-                if (a.gate != nullptr) {
-                    load_cond(static_cast<const char *>(a.gate) + cond, a.cond_f32, piece(v), u);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[v][i] *= u[i];
-                }
+                if (!kAhead) load_post(v);
+                multiply(a.post_gain, x[v], post_gain);
+                add(a.post_bias, x[v], post_bias);
+                multiply(a.scale, x[v], scale);
+                multiply(a.gate, x[v], gate);
             }
     }
 #pragma unroll
@@ -140,27 +167,13 @@ __global__ __launch_bounds__(256) void residual_norm_kernel(ResidualNorm a)
 #pragma unroll
     for (int v = 0; v < V; ++v)
         if (there(v)) {
-            float u[8];
-            if (a.gain != nullptr) {
-                load_eight(a.gain + piece(v), u);
+            if (!kAhead) load_pre(v);
+            multiply(a.gain, x[v], gain);
+            add(a.bias, x[v], bias);
+            if (a.mod_scale != nullptr)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[v][i] *= u[i];
-            }
-            if (a.bias != nullptr) {
-                load_eight(a.bias + piece(v), u);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[v][i] += u[i];
-            }
-            if (a.mod_scale != nullptr) {
-                load_cond(static_cast<const char *>(a.mod_scale) + cond, a.cond_f32, piece(v), u);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[v][i] = fmaf(x[v][i], u[i], x[v][i]);
-            }
-            if (a.mod_shift != nullptr) {
-                load_cond(static_cast<const char *>(a.mod_shift) + cond, a.cond_f32, piece(v), u);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[v][i] += u[i];
-            }
+                for (int i = 0; i < 8; ++i) x[v][i] = fmaf(x[v][i], mod_scale[i], x[v][i]);
+            add(a.mod_shift, x[v], mod_shift);
             store_eight<HF>(static_cast<char *>(a.h) + at * (HF ? 4 : 2), piece(v), x[v]);
         }
 }
@@ -168,9 +181,12 @@ __global__ __launch_bounds__(256) void residual_norm_kernel(ResidualNorm a)
 template <int LANES, int V, bool XF, bool YF, bool HF>
 hipError_t launch(const ResidualNorm &a, hipStream_t stream)
 {
-    residual_norm_kernel<LANES, V, XF, YF, HF><<<dim3((unsigned)(((long long)a.M * LANES + 255) / 256)), 256, 0, stream>>>(a);
+    if (LANES == 0) residual_norm_kernel<LANES, V, XF, YF, HF><<<dim3(a.M), dim3((a.C / 8 + 63) / 64 * 64), 0, stream>>>(a);
+    else residual_norm_kernel<LANES, V, XF, YF, HF><<<dim3((unsigned)(((long long)a.M * LANES + 255) / 256)), 256, 0, stream>>>(a);
     return hipGetLastError();
 }
+// Lanes by the row's length: few enough that all have work, and no more than a wave where a lane can hold its part (2048 channels: 90 us for 30000 rows, 94 with a block for each; more pieces a lane than
+// four cost waves: 8191 rows of 2560 channels with everything given 68 us with five, 56 with a block).
 template <bool XF, bool YF, bool HF>
 hipError_t launch(const ResidualNorm &a, hipStream_t stream)
 {
@@ -179,8 +195,7 @@ hipError_t launch(const ResidualNorm &a, hipStream_t stream)
     if (a.C <= 512) return launch<64, 1, XF, YF, HF>(a, stream);
     if (a.C <= 1024) return launch<64, 2, XF, YF, HF>(a, stream);
     if (a.C <= 2048) return launch<64, 4, XF, YF, HF>(a, stream);
-    if (a.C <= 4096) return launch<256, 2, XF, YF, HF>(a, stream);
-    return launch<256, 4, XF, YF, HF>(a, stream);
+    return launch<0, 1, XF, YF, HF>(a, stream);
 }
 
 }  // namespace
