@@ -942,7 +942,7 @@ bool valid_packed(int T, int S, int seqs, int max_q, int max_kv, int q_heads, in
 {
     return T >= 0 && S >= 0 && seqs >= 0 && seqs <= 65535 && max_q >= 0 && max_kv >= 0 && max_kv <= (1 << 30) && (d == 64 || d == 128) && kv_heads >= 1 && kv_heads <= 65535 &&
            q_heads >= kv_heads && q_heads <= 65535 && q_heads % kv_heads == 0 && (long long)max_q * (q_heads / kv_heads) <= (1 << 30) &&
-           (long long)seqs * kv_heads * qvggt::attention_div_up((long long)max_q * (q_heads / kv_heads), qvggt::kAttentionTile) <= qvggt::kAttentionMostBlocks;
+           (long long)seqs * kv_heads * qvggt::attention_div_up((long long)max_q * (q_heads / kv_heads), 32) <= qvggt::kAttentionMostBlocks;
 }
 }  // namespace
 
@@ -971,7 +971,7 @@ int qvggt_heads_norm_rope(const void *Q, const void *K, int dtype, int T, long l
 
 size_t qvggt_attention_workspace_bytes(int T, int seqs, int max_q, int max_kv, int q_heads, int kv_heads, int d)
 {
-    return valid_packed(T, 0, seqs, max_q, max_kv, q_heads, kv_heads, d) ? qvggt::attention_plan(seqs, max_q, max_kv, q_heads, kv_heads, d).bytes : 0;
+    return valid_packed(T, 0, seqs, max_q, max_kv, q_heads, kv_heads, d) ? qvggt::attention_workspace(seqs, max_q, max_kv, q_heads, kv_heads, d) : 0;
 }
 
 int qvggt_attention(const void *Q, const void *K, const void *V, int dtype, int T, int S, long long q_stride, long long k_stride, long long v_stride, int q_heads, int kv_heads, int d,
@@ -984,7 +984,7 @@ int qvggt_attention(const void *Q, const void *K, const void *V, int dtype, int 
         return QVGGT_ERR_SHAPE;
     if (!std::isfinite(scale) || (causal != 0 && causal != 1)) return QVGGT_ERR_ARG;
     if (T == 0 || seqs == 0 || max_q == 0) return QVGGT_OK;
-    const size_t need = qvggt::attention_plan(seqs, max_q, max_kv, q_heads, kv_heads, d).bytes;
+    const size_t need = qvggt::attention_workspace(seqs, max_q, max_kv, q_heads, kv_heads, d);
     if (!Q || !q_starts || !kv_starts || !out || (max_kv > 0 && (!K || !V)) || (need > 0 && !workspace)) return QVGGT_ERR_NULL;
     if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || q_stride % 8 != 0 || k_stride % 8 != 0 || v_stride % 8 != 0 || !aligned4(q_starts) || !aligned4(kv_starts) ||
         !aligned4(kv_lens) || !aligned16(out) || !aligned16(workspace))

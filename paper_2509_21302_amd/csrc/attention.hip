@@ -1,13 +1,13 @@
 // Attention of packed sequences over bf16 keys and values:   out[i, h] = sum_j softmax_j(scale <q[i, h], k[j, h']>) v[j, h'].
 //
-// Rows are the query tokens of a sequence times the query heads that share a key head; a wave has a tile of 32.  Scores are keys x queries and results channels x queries (both
-// v_mfma_f32_32x32x16_bf16): a lane's accumulators are 16 keys of one row, which is what its part of the second product's right operand is made of, if the 16 keys of a step come in the order
-//     element j of lane l  =  key 8 (j / 4) + 4 (l / 32) + j % 4
-// in both operands.  So nothing moves between lanes but a maximum and a sum for every row, and a row's factor is a lane's.  The values' operand has that order from LDS reads that
-// transpose: four keys of sixteen channels a group of sixteen lanes.
+// Rows are the query tokens of a sequence times the query heads that share a key head; a wave has tiles of M = 16 or 32 of them.  Scores are keys x queries and results channels x queries, both
+// v_mfma_f32_16x16x32_bf16 or v_mfma_f32_32x32x16_bf16.  With G = 64 / M groups of lanes, group g of a lane, its accumulators of consecutive tiles of keys are the keys
+//     number f  =  key 4 G (f / 4) + 4 g + f % 4
+// of one row, and eight of them are what its part of the second product's right operand is made of, if the 8 G keys of a step come in that order in both operands.  So nothing moves between lanes but
+// a maximum and a sum for every row, and a row's factor is a lane's.  The values' operand has that order from LDS reads that transpose: four keys of sixteen channels a group of sixteen lanes.
 //
 // Keys and values go straight from memory into LDS, 16 bytes a lane, rows as they are.  A row's 16-byte pieces change places by its number (the source address does that), so that reads
-// of 32 rows of keys, and of four rows of values, touch every bank as often as any other.
+// of rows of keys, and of a few rows of values, touch every bank as often as any other.
 //
 // The running maximum of a row is raised when one of its scores exceeds it by more than 2^8 in weight: weights are at most 2^8 then, and sums are multiplied by a factor in few steps.  Weights
 // are rounded to bf16 (to nearest), for the product and for the sum that it is divided by alike.  A row starts from a maximum of -3e38, so that rows that see nothing end with a sum of 0.
@@ -23,6 +23,7 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef short short4v __attribute__((ext_vector_type(4)));
+typedef float float4v __attribute__((ext_vector_type(4)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 union Operand {
     uint4 u;
@@ -62,122 +63,160 @@ __device__ inline Sequence sequence_of(const Attention &a, int b)
 __device__ inline int visible(const Attention &a, const Sequence &s, int i) { return a.causal ? min(max(s.len - s.total + i + 1, 0), s.limit) : s.limit; }
 
 // ---- how rows lie in LDS
-template <int D>
+template <int D, int M>
 struct Rows {
     static constexpr int kBytes = 2 * D, kPieces = D / 8, kPerTransfer = 64 / kPieces;      // rows that one transfer of a wave brings
-    // Place of piece c of a row: of keys, 32 rows are read at one piece; of values, four rows at four pieces
+    // Place of piece c of a row.  Of keys, sixteen lanes read as many rows at one piece; of values, thirty-two lanes read eight rows at two pieces (M = 16) or four rows at four
     __device__ static int key_piece(int row, int c) { return D == 128 ? c ^ (row & 15) : c ^ (row >> 1 & 7); }
-    __device__ static int value_piece(int row, int c) { return D == 128 ? c ^ (row & 3) << 2 : c ^ (row >> 1 & 1) << 2; }
+    __device__ static int value_piece(int row, int c)
+    {
+        if (M == 16) return D == 128 ? c ^ (row & 7) << 1 : c ^ (row >> 1 & 3) << 1;
+        return D == 128 ? c ^ (row & 3) << 2 : c ^ (row >> 1 & 1) << 2;
+    }
 };
 
-template <int D>
-struct Wave {
-    typedef Rows<D> R;
-    static constexpr int kSteps = D / 16, kTiles = D / 32;
-    Operand q[kSteps];
-    float16v o[kTiles];
-    float top, sum;
-    int lane, half, end;            // keys that the lane's row sees
+__device__ inline float4v product(const Operand &a, const Operand &b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.b, b.b, c, 0, 0, 0); }
+__device__ inline float16v product(const Operand &a, const Operand &b, float16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.b, b.b, c, 0, 0, 0); }
 
-    __device__ void begin(const Cut &w, const Sequence &s, int head, int row, int rows, int lane_)
+// A wave's NQ tiles of M rows
+template <int D, int M, int NQ>
+struct Wave {
+    typedef Rows<D, M> R;
+    typedef std::conditional_t<M == 16, float4v, float16v> Sums;
+    static constexpr int kGroups = 64 / M, kSums = M / kGroups, kSteps = D / (8 * kGroups), kTiles = D / M, kKeys = 8 * kGroups;    // kSums: of a lane in a tile; kKeys: of an operand of values
+    Operand q[NQ][kSteps];
+    Sums o[kTiles][NQ];
+    float top[NQ], sum[NQ];
+    int lane, g, end[NQ];           // keys that the lane's rows see
+
+    // The rows' queries on their way; take() waits for them, and for everything that was asked for since.
+    __device__ void load(const Cut &w, const Sequence &s, int head, int row0, int rows, int lane_)
     {
         lane = lane_;
-        half = lane >> 5;
-        top = kNone;
-        sum = 0.0f;
-        end = row < rows ? visible(w.a, s, row / w.group) : 0;
-        const int r = min(row, rows - 1), i = r / w.group;
-        const uint16_t *const from = w.a.q + (long long)(s.q0 + i) * w.a.q_stride + (head * w.group + r - i * w.group) * D + 8 * half;
+        g = lane / M;
 #pragma unroll
-        for (int k = 0; k < kSteps; ++k) {
-            q[k].u = *reinterpret_cast<const uint4 *>(from + 16 * k);
+        for (int n = 0; n < NQ; ++n) {
+            const int row = row0 + M * n + lane % M, r = min(row, rows - 1), i = r / w.group;
+            top[n] = kNone;
+            sum[n] = 0.0f;
+            end[n] = row < rows ? visible(w.a, s, i) : 0;
+            const uint16_t *const from = w.a.q + (long long)(s.q0 + i) * w.a.q_stride + (head * w.group + r - i * w.group) * D + 8 * g;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) q[k].w[j] = (q[k].w[j] & w.keep) ^ w.flip;
+            for (int k = 0; k < kSteps; ++k) q[n][k].u = *reinterpret_cast<const uint4 *>(from + 8 * kGroups * k);
         }
+    }
+    __device__ void take(const Cut &w)
+    {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) q[n][k].w[j] = (q[n][k].w[j] & w.keep) ^ w.flip;
 #pragma unroll
         for (int c = 0; c < kTiles; ++c)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[c][i] = 0.0f;
+            for (int n = 0; n < NQ; ++n) o[c][n] = Sums{};
     }
-    // Scores of NK x 32 keys at `keys` (LDS).
+    // Scores of NK tiles of M keys at `keys` (LDS).
     template <int NK>
-    __device__ void scores(const char *keys, float16v (&x)[NK]) const
+    __device__ void scores(const char *keys, Sums (&x)[NK][NQ]) const
     {
-        const int row = lane & 31;
+        const int row = lane % M;
 #pragma unroll
         for (int k = 0; k < kSteps; ++k)
 #pragma unroll
-            for (int n = 0; n < NK; ++n) {
+            for (int m = 0; m < NK; ++m) {
                 Operand a;
-                a.u = *reinterpret_cast<const uint4 *>(keys + (row * R::kBytes + R::key_piece(row, 2 * k + half) * 16) + 32 * n * R::kBytes);
-                x[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.b, q[k].b, k == 0 ? float16v{} : x[n], 0, 0, 0);
+                a.u = *reinterpret_cast<const uint4 *>(keys + (row * R::kBytes + R::key_piece(row, kGroups * k + g) * 16) + M * m * R::kBytes);
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) x[m][n] = product(a, q[n][k], k == 0 ? Sums{} : x[m][n]);
             }
     }
-    // Unseen keys of NK x 32 from number t on.
+    // Unseen keys of NK tiles from number t on.
     template <int NK>
-    __device__ void hide(float16v (&x)[NK], int t) const
+    __device__ void hide(Sums (&x)[NK][NQ], int t) const
     {
-        const int seen = end - t - 4 * half;
 #pragma unroll
-        for (int k = 0; k < NK; ++k)
+        for (int n = 0; n < NQ; ++n) {
+            const int seen = end[n] - t - 4 * g;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[k][i] = 32 * k + 8 * (i / 4) + i % 4 < seen ? x[k][i] : -INFINITY;
-    }
-    // The largest score of a row.
-    template <int NK>
-    __device__ static float largest(const float16v (&x)[NK])
-    {
-        float m = fmaxf(x[0][0], x[0][1]);
+            for (int m = 0; m < NK; ++m)
 #pragma unroll
-        for (int k = 0; k < NK; ++k)
-#pragma unroll
-            for (int i = k == 0 ? 2 : 0; i < 16; i += 2) m = fmaxf(fmaxf(m, x[k][i]), x[k][i + 1]);
-        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
-        return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-    }
-    // ... and the maximum raised to it where that is called for.
-    __device__ void raise(float m, float scale2)
-    {
-        if (__builtin_amdgcn_ballot_w64((m - top) * scale2 > kSlack)) {
-            const float next = fmaxf(top, m), f = __builtin_amdgcn_exp2f((top - next) * scale2);
-            top = next;
-            sum *= f;
-#pragma unroll
-            for (int c = 0; c < kTiles; ++c)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[c][i] *= f;
+                for (int i = 0; i < kSums; ++i) x[m][n][i] = M * m + 4 * kGroups * (i / 4) + i % 4 < seen ? x[m][n][i] : -INFINITY;
         }
     }
-    // Weights of NK x 32 keys, as operands of 16 keys each.
+    // The largest scores of the rows.
     template <int NK>
-    __device__ void weights(const float16v (&x)[NK], float scale2, Operand (&p)[2 * NK])
+    __device__ static void largest(const Sums (&x)[NK][NQ], float (&top)[NQ])
     {
-        const float off = top * scale2;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            float m = fmaxf(x[0][n][0], x[0][n][1]);
+#pragma unroll
+            for (int k = 0; k < NK; ++k)
+#pragma unroll
+                for (int i = k == 0 ? 2 : 0; i < kSums; i += 2) m = fmaxf(fmaxf(m, x[k][n][i]), x[k][n][i + 1]);
+            if (M == 16) {
+                const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+                m = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+            }
+            const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+            top[n] = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+        }
+    }
+    // ... and the maxima raised to them where that is called for.
+    __device__ void raise(const float (&m)[NQ], float scale2)
+    {
+        bool higher = false;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) higher |= (m[n] - top[n]) * scale2 > kSlack;
+        if (__builtin_amdgcn_ballot_w64(higher)) {
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                const float next = fmaxf(top[n], m[n]), f = __builtin_amdgcn_exp2f((top[n] - next) * scale2);
+                top[n] = next;
+                sum[n] *= f;
+#pragma unroll
+                for (int c = 0; c < kTiles; ++c)
+#pragma unroll
+                    for (int i = 0; i < kSums; ++i) o[c][n][i] *= f;
+            }
+        }
+    }
+    // Weights of NK tiles of keys, as operands.
+    template <int NK>
+    __device__ void weights(const Sums (&x)[NK][NQ], float scale2, Operand (&p)[NK * M / kKeys][NQ])
+    {
         bf16x2 one;
         one[0] = one[1] = (__bf16)1.0f;
 #pragma unroll
-        for (int k = 0; k < NK; ++k)
+        for (int n = 0; n < NQ; ++n) {
+            const float off = top[n] * scale2;
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                const float a = __builtin_amdgcn_exp2f(fmaf(x[k][i], scale2, -off)), b = __builtin_amdgcn_exp2f(fmaf(x[k][i + 1], scale2, -off));
-                const uint32_t both = pack_bf16x2(a, b);
-                p[2 * k + i / 8].w[i % 8 / 2] = both;
-                sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, both), one, sum, false);
-            }
+            for (int k = 0; k < NK; ++k)
+#pragma unroll
+                for (int i = 0; i < kSums; i += 2) {
+                    const float a = __builtin_amdgcn_exp2f(fmaf(x[k][n][i], scale2, -off)), b = __builtin_amdgcn_exp2f(fmaf(x[k][n][i + 1], scale2, -off));
+                    const uint32_t both = pack_bf16x2(a, b);
+                    p[(k * kSums + i) / 8][n].w[(k * kSums + i) % 8 / 2] = both;
+                    sum[n] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, both), one, sum[n], false);
+                }
+        }
     }
-    // 16 keys' values at `values` (LDS)
-    __device__ void add(const char *values, const Operand &p)
+    // The values of an operand's keys at `values` (LDS).
+    __device__ void add(const char *values, const Operand (&p)[NQ])
     {
-        const int i = lane & 15, row = 4 * half + (i >> 2);
+        const int i = lane & 15, row = 4 * g + (i >> 2);
 #pragma unroll
         for (int c = 0; c < kTiles; ++c) {
-            const int piece = R::value_piece(row, 4 * c + 2 * (lane >> 4 & 1) + (i >> 1 & 1));
-            const char *const at = values + row * R::kBytes + piece * 16 + 8 * (i & 1);
+            const char *const at = values + row * R::kBytes + R::value_piece(row, M / 8 * c + (M == 32 ? 2 * (lane >> 4 & 1) : 0) + (i >> 1 & 1)) * 16 + 8 * (i & 1);
             Operand a;
 #pragma unroll
             for (int j = 0; j < 2; ++j)
-                a.s[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v *)(const_cast<char *>(at) + 8 * j * R::kBytes));
-            o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.b, p.b, o[c], 0, 0, 0);
+                a.s[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v *)(const_cast<char *>(at) + 4 * kGroups * j * R::kBytes));
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) o[c][n] = product(a, p[n], o[c][n]);
         }
     }
     // A value that is no number touches only the rows that see it: where `keys` rows of values have one and some rows of the wave do not see all of those keys, it is added to the rows that
@@ -188,19 +227,28 @@ struct Wave {
 #pragma unroll
             for (int c = 0; c < kTiles; ++c)
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const uint2 v = *reinterpret_cast<const uint2 *>(values + key * R::kBytes + R::value_piece(key, 4 * c + g) * 16 + 8 * half);
+                for (int f = 0; f < kSums; f += 4) {
+                    const int channel = M * c + kGroups * f + 4 * g;            // and the three behind it
+                    const uint2 v = *reinterpret_cast<const uint2 *>(values + key * R::kBytes + R::value_piece(key, channel / 8) * 16 + 2 * (channel & 4));
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const uint32_t bits = (i & 2 ? v.y : v.x) >> 16 * (i & 1) << 16;
-                        if ((bits & 0x7f800000u) == 0x7f800000u && t + key < end) o[c][4 * g + i] += __uint_as_float(bits);
+                        if ((bits & 0x7f800000u) == 0x7f800000u)
+#pragma unroll
+                            for (int n = 0; n < NQ; ++n)
+                                if (t + key < end[n]) o[c][n][f + i] += __uint_as_float(bits);
                     }
                 }
     }
-    // A row's parts of the two lanes that have it.
-    __device__ float total() const
+    // A row's parts of the lanes that have it.
+    __device__ float total(int n) const
     {
-        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+        float s = sum[n];
+        if (M == 16) {
+            const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(s), __float_as_uint(s), false, false);
+            s = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+        }
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(s), __float_as_uint(s), false, false);
         return __uint_as_float(r[0]) + __uint_as_float(r[1]);
     }
 };
@@ -234,14 +282,15 @@ __device__ inline void take_out_no_numbers(char *values, int bytes, int first, i
 
 // ---- from memory into LDS
 __device__ inline uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)p; }
-// One transfer: rows first .. first + kPerTransfer - 1 of those at `from` (rows past `most` are read as that one), to `lds` + their place
-template <int D, bool KEYS>
+// One transfer: rows first .. first + kPerTransfer - 1 of those at `from` (rows past `most` are read as that one), to `lds` + their place.  ONCE: of rows that nobody else reads, past the caches.
+template <class R, bool KEYS, bool ONCE>
 __device__ inline void transfer(const uint16_t *from, long long stride, int first, int most, uint32_t lds, int lane)
 {
-    typedef Rows<D> R;
     const int row = first + lane / R::kPieces, c = lane % R::kPieces;
     const int piece = KEYS ? R::key_piece(row, c) : R::value_piece(row, c);
-    dma16((uint32_t)(min(row, most) * (int)stride * 2 + piece * 16), from, lds + first * R::kBytes);
+    const uint32_t at = (uint32_t)(min(row, most) * (int)stride * 2 + piece * 16);
+    if (ONCE) dma16_once(at, from, lds + first * R::kBytes);
+    else dma16(at, from, lds + first * R::kBytes);
 }
 
 template <int D>
@@ -277,24 +326,25 @@ __device__ inline void pace()
 template <int D>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attention_own_rows_kernel(Cut w)
 {
-    typedef Rows<D> R;
+    typedef Rows<D, 32> R;
     constexpr int kKeys = 64, kTile = kKeys * R::kBytes, kEach = kKeys / R::kPerTransfer / 4;
     __shared__ __align__(16) char area[4 * kTile];          // two tiles of keys, two of values
     char *const keys = area, *const values = area + 2 * kTile;
     const Attention &a = w.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // Heads first, parts next, then tiles from the last one on, where rows see most, sequences last: blocks that run together have keys in common (those of a head on one of the eight dies, where
-    // heads are a multiple of eight), and a sequence's longest blocks begin first
-    const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, place = rest % (w.tiles * w.splits), b = rest / (w.tiles * w.splits);
+    // Heads first, then tiles from the last one on, where rows see most, then sequences, parts of the keys last: blocks that run together have keys in common (those of a head on one of the eight
+    // dies, where heads are a multiple of eight), a sequence's longest blocks begin first, and a part that has less to do than another is on all dies alike (a prompt of 16384 tokens in two parts,
+    // 16 heads on 4: 613 us for 884 with parts side by side)
+    const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, place = rest % w.tiles, b = rest / w.tiles % a.seqs, split = rest / w.tiles / a.seqs;
     const Sequence seq = sequence_of(a, b);
-    const int rows = seq.n * w.group, tile = (rows + 127) / 128 - 1 - place / w.splits, split = place % w.splits;
+    const int rows = seq.n * w.group, tile = (rows + 127) / 128 - 1 - place;
     if (tile < 0) return;
     const int row0 = tile * 128, row = row0 + 32 * wave + (lane & 31), rows_end = min(rows, row0 + 128);
     const int last = visible(a, seq, (rows_end - 1) / w.group), full = visible(a, seq, row0 / w.group);        // keys that some row of the block sees, and that all see
     const int t0 = split * w.chunk, stop = min(last, t0 + w.chunk), steps = (stop - t0 + kKeys - 1) / kKeys;
     if (split > 0 && t0 >= last) return;
-    Wave<D> r;
-    r.begin(w, seq, head, row, rows, lane);
+    Wave<D, 32, 1> r;
+    r.load(w, seq, head, row0 + 32 * wave, rows, lane);
     const uint16_t *const k = a.k + (long long)(seq.k0 + t0) * a.k_stride + head * D, *const v = a.v + (long long)(seq.k0 + t0) * a.v_stride + head * D;
     // A lane's place in this wave's transfers of a tile: the keys' pieces change with the row, the values' do not from transfer to transfer
     uint32_t from_key[kEach], from_value;
@@ -314,7 +364,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attention_own_rows_kerne
             for (int i = 0; i < kEach; ++i) dma16(from_key[i], from, to + i * R::kPerTransfer * R::kBytes);
         } else
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) transfer<D, true>(from, a.k_stride, first + i * R::kPerTransfer, last - 1 - t0 - step * kKeys, lds_address(keys) + buffer * kTile, lane);
+            for (int i = 0; i < kEach; ++i) transfer<R, true, false>(from, a.k_stride, first + i * R::kPerTransfer, last - 1 - t0 - step * kKeys, lds_address(keys) + buffer * kTile, lane);
     };
     auto bring_values = [&](int step, int buffer) {
         const uint16_t *const from = v + (long long)step * kKeys * a.v_stride;
@@ -324,27 +374,31 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attention_own_rows_kerne
             for (int i = 0; i < kEach; ++i) dma16(from_value, from + (long long)i * R::kPerTransfer * a.v_stride, to + i * R::kPerTransfer * R::kBytes);
         } else
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) transfer<D, false>(from, a.v_stride, first + i * R::kPerTransfer, last - 1 - t0 - step * kKeys, lds_address(values) + buffer * kTile, lane);
+            for (int i = 0; i < kEach; ++i) transfer<R, false, false>(from, a.v_stride, first + i * R::kPerTransfer, last - 1 - t0 - step * kKeys, lds_address(values) + buffer * kTile, lane);
     };
     auto arrived = [] {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
     };
     if (steps > 0) {
-        // While a step's weights are made the next one's scores are multiplied, and its maximum is looked for while this one's values are: keys are a step ahead of values
-        float16v x[2], y[2];
-        Operand p[4];
         bring_keys(0, 0);
         bring_values(0, 0);
+    }
+    r.take(w);
+    if (steps > 0) {
+        // While a step's weights are made the next one's scores are multiplied, and its maximum is looked for while this one's values are: keys are a step ahead of values
+        float16v x[2][1], y[2][1];
+        Operand p[4][1];
         arrived();
         r.scores(keys, x);
         if (steps > 1) bring_keys(1, 1);
-        float m = r.largest(x);
+        float m[1];
+        r.largest(x, m);
         arrived();
         // Steps that every row of the block sees, two at a time; behind each of them there is another
         const int plain = min(max(full - t0, 0) / kKeys, steps - 1) & ~1;
         int step = 0;
-        auto both = [&](auto parity, float16v(&x)[2], float16v(&y)[2]) {
+        auto both = [&](auto parity, float16v(&x)[2][1], float16v(&y)[2][1]) {
             constexpr int kHere = decltype(parity)::value, kNext = kHere ^ 1;
             if (step + 2 < steps) bring_keys(step + 2, kHere);
             bring_values(step + 1, kNext);
@@ -353,7 +407,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attention_own_rows_kerne
             r.weights(x, w.scale2, p);
 #pragma unroll
             for (int i = 0; i < 4; ++i) r.add(values + kHere * kTile + 16 * i * R::kBytes, p[i]);
-            m = r.largest(y);
+            r.largest(y, m);
             ++step;
             pace<D>();
             arrived();
@@ -375,7 +429,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attention_own_rows_kerne
             bool bad = false;
             if (t + kKeys > full) {
                 r.hide(x, t);
-                m = r.largest(x);
+                r.largest(x, m);
                 bad = __syncthreads_or(find_no_numbers(mine, kTile, threadIdx.x, 256));
             }
             r.raise(m, w.scale2);
@@ -389,46 +443,51 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attention_own_rows_kerne
 #pragma unroll
             for (int i = 0; i < 4; ++i) r.add(mine + 16 * i * R::kBytes, p[i]);
             if (more) {
-                x[0] = y[0];
-                x[1] = y[1];
-                m = r.largest(x);
+                x[0][0] = y[0][0];
+                x[1][0] = y[1][0];
+                r.largest(x, m);
             }
             arrived();
         }
     }
-    const float total = r.total();
-    if (row >= rows) return;
+    const float total = r.total(0);
     if (w.splits == 1) {
         const float f = total != 0.0f ? 1.0f / total : 0.0f;        // (a row that is no number has a total that is none)
         const int i = row / w.group;
         uint16_t *const to = a.out + ((long long)(seq.q0 + i) * a.q_heads + head * w.group + row - i * w.group) * D;
+        // Of sixteen channels, of which the two lanes of a row have fours in turn, each comes to have eight neighbouring ones
 #pragma unroll
         for (int c = 0; c < D / 32; ++c)
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
-                *reinterpret_cast<uint2 *>(to + 32 * c + 8 * g + 4 * r.half) =
-                    make_uint2(pack_bf16x2(r.o[c][4 * g] * f, r.o[c][4 * g + 1] * f), pack_bf16x2(r.o[c][4 * g + 2] * f, r.o[c][4 * g + 3] * f));
-    } else {
+            for (int e = 0; e < 16; e += 8) {
+                uint32_t word[4];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const auto s = __builtin_amdgcn_permlane32_swap(pack_bf16x2(r.o[c][0][e + 2 * j] * f, r.o[c][0][e + 2 * j + 1] * f),
+                                                                    pack_bf16x2(r.o[c][0][e + 4 + 2 * j] * f, r.o[c][0][e + 4 + 2 * j + 1] * f), false, false);
+                    word[j] = s[0];
+                    word[2 + j] = s[1];
+                }
+                if (row < rows) *reinterpret_cast<uint4 *>(to + 32 * c + 2 * e + 8 * r.g) = make_uint4(word[0], word[1], word[2], word[3]);
+            }
+    } else if (row < rows) {
         float *const to = w.partials + partial_row(w, b, head, row, split) * kPartial<D>;
 #pragma unroll
         for (int c = 0; c < D / 32; ++c)
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
-#pragma unroll
-                for (int i = 0; i < 4; i += 2)
-                    *reinterpret_cast<float2 *>(to + 32 * c + 8 * g + 4 * r.half + i) = make_float2(r.o[c][4 * g + i], r.o[c][4 * g + i + 1]);
-        if (r.half == 0) *reinterpret_cast<float2 *>(to + D) = make_float2(r.top * w.scale2, total);
+            for (int e = 0; e < 16; e += 2) *reinterpret_cast<float2 *>(to + 32 * c + 8 * (e / 4) + 4 * r.g + e % 4) = make_float2(r.o[c][0][e], r.o[c][0][e + 1]);
+        if (r.g == 0) *reinterpret_cast<float2 *>(to + D) = make_float2(r.top[0] * w.scale2, total);
     }
 }
 
 // ---- few rows (32 at most): the waves of a block share them and go through keys of their own, 32 at a time, brought into LDS by each for itself
-template <int D>
-__global__ __launch_bounds__(256, 2) void attention_few_rows_kernel(Cut w)
+template <int D, int NQ, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 2 : 1) void attention_few_rows_kernel(Cut w)
 {
-    typedef Rows<D> R;
+    typedef Rows<D, 16> R;
     constexpr int kKeys = 32, kTile = kKeys * R::kBytes, kEach = kKeys / R::kPerTransfer;
-    __shared__ __align__(16) char area[4][2][kTile];
-    __shared__ float tops[4][32], totals[4][32];
+    extern __shared__ __align__(16) char few_area[];        // a tile of keys and one of values for every wave
+    __shared__ float tops[WAVES][16 * NQ], totals[WAVES][16 * NQ];
     const Attention &a = w.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, split = rest % w.splits, b = rest / w.splits;
@@ -437,36 +496,39 @@ __global__ __launch_bounds__(256, 2) void attention_few_rows_kernel(Cut w)
     if (rows == 0) return;
     const int last = visible(a, seq, seq.n - 1), full = visible(a, seq, 0), t0 = split * w.chunk, stop = min(last, t0 + w.chunk);
     if (split > 0 && t0 >= last) return;
-    Wave<D> r;
+    Wave<D, 16, NQ> r;
     const uint16_t *const k = a.k + (long long)seq.k0 * a.k_stride + head * D, *const v = a.v + (long long)seq.k0 * a.v_stride + head * D;
-    char *const keys = area[wave][0], *const values = area[wave][1];
+    char *const keys = few_area + wave * 2 * kTile, *const values = keys + kTile;
     auto bring_keys = [&](int t) {
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) transfer<D, true>(k + (long long)t * a.k_stride, a.k_stride, i * R::kPerTransfer, last - 1 - t, lds_address(keys), lane);
+        for (int i = 0; i < kEach; ++i) transfer<R, true, true>(k + (long long)t * a.k_stride, a.k_stride, i * R::kPerTransfer, last - 1 - t, lds_address(keys), lane);
     };
     auto bring_values = [&](int t) {
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) transfer<D, false>(v + (long long)t * a.v_stride, a.v_stride, i * R::kPerTransfer, last - 1 - t, lds_address(values), lane);
+        for (int i = 0; i < kEach; ++i) transfer<R, false, true>(v + (long long)t * a.v_stride, a.v_stride, i * R::kPerTransfer, last - 1 - t, lds_address(values), lane);
     };
-    r.begin(w, seq, head, lane & 31, rows, lane);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // the queries: from here on only transfers are counted
+    r.load(w, seq, head, 0, rows, lane);
     int t = t0 + kKeys * wave;
     if (t < stop) {
         bring_keys(t);
         bring_values(t);
     }
-    for (; t < stop; t += 4 * kKeys) {
-        const bool more = t + 4 * kKeys < stop;
+    r.take(w);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // the queries and the first tile: from here on only transfers are counted
+    for (; t < stop; t += WAVES * kKeys) {
+        const bool more = t + WAVES * kKeys < stop;
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kEach) : "memory");        // the keys; the values are on their way
         lanes_exchange_fence();
-        float16v x[1];
-        Operand p[2];
+        float4v x[2][NQ];
+        Operand p[1][NQ];
+        float m[NQ];
         r.scores(keys, x);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (more) bring_keys(t + 4 * kKeys);
+        if (more) bring_keys(t + WAVES * kKeys);
         const bool masked = t + kKeys > full;
         if (masked) r.hide(x, t);
-        r.raise(r.largest(x), w.scale2);
+        r.largest(x, m);
+        r.raise(m, w.scale2);
         r.weights(x, w.scale2, p);
         if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kEach) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -478,37 +540,35 @@ __global__ __launch_bounds__(256, 2) void attention_few_rows_kernel(Cut w)
             lanes_exchange_fence();
         }
         r.add(values, p[0]);
-        r.add(values + 16 * R::kBytes, p[1]);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (more) bring_values(t + 4 * kKeys);
+        if (more) bring_values(t + WAVES * kKeys);
     }
     // The waves' sums, in the LDS that held their tiles: rows of D floats, their pieces of four in an order by the row
-    const float total = r.total();
-    __syncthreads();
     constexpr int kFours = D / 4;
-    float *const mine = reinterpret_cast<float *>(area[wave][0]);
-    const int here = lane & 31;
+    float *const mine = reinterpret_cast<float *>(keys);
+    __syncthreads();
 #pragma unroll
-    for (int c = 0; c < D / 32; ++c)
+    for (int n = 0; n < NQ; ++n) {
+        const int here = 16 * n + (lane & 15);
+        const float total = r.total(n);
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
-            *reinterpret_cast<float4 *>(mine + here * D + ((8 * c + 2 * g + r.half) ^ (here & (kFours - 1))) * 4) =
-                make_float4(r.o[c][4 * g], r.o[c][4 * g + 1], r.o[c][4 * g + 2], r.o[c][4 * g + 3]);
-    if (lane < 32) {
-        tops[wave][lane] = r.top;
-        totals[wave][lane] = total;
+        for (int c = 0; c < D / 16; ++c) *reinterpret_cast<float4 *>(mine + here * D + ((4 * c + r.g) ^ (here & (kFours - 1))) * 4) = make_float4(r.o[c][n][0], r.o[c][n][1], r.o[c][n][2], r.o[c][n][3]);
+        if (r.g == 0) {
+            tops[wave][here] = r.top[n];
+            totals[wave][here] = total;
+        }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < rows * kFours; i += 256) {
+    for (int i = threadIdx.x; i < rows * kFours; i += 64 * WAVES) {
         const int row = i / kFours, c = i % kFours;
         float top = kNone, all = 0.0f;
 #pragma unroll
-        for (int n = 0; n < 4; ++n) top = fmaxf(top, tops[n][row]);
+        for (int n = 0; n < WAVES; ++n) top = fmaxf(top, tops[n][row]);
         float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
+        for (int n = 0; n < WAVES; ++n) {
             const float f = __builtin_amdgcn_exp2f((tops[n][row] - top) * w.scale2);
-            const float4 y = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(area[n][0]) + row * D + (c ^ (row & (kFours - 1))) * 4);
+            const float4 y = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(few_area + n * 2 * kTile) + row * D + (c ^ (row & (kFours - 1))) * 4);
             all = fmaf(f, totals[n][row], all);
             x = make_float4(fmaf(f, y.x, x.x), fmaf(f, y.y, x.y), fmaf(f, y.z, x.z), fmaf(f, y.w, x.w));
         }
@@ -526,28 +586,45 @@ __global__ __launch_bounds__(256, 2) void attention_few_rows_kernel(Cut w)
     }
 }
 
-// ---- the parts of a row put together: 16 lanes have a row
+// ---- the parts of a row put together: 16 lanes have a row.  Every lane finds the factors of some of the parts, which all need
 template <int D>
 __global__ __launch_bounds__(256) void attention_join_kernel(Cut w)
 {
     constexpr int C = D / 16;
+    __shared__ float factors[16][kAttentionMostParts];
     const Attention &a = w.a;
-    const int first = (threadIdx.x & 15) * C, blocks = (a.max_q * w.group + 15) / 16;
+    const int lane = threadIdx.x & 15, first = lane * C, blocks = (a.max_q * w.group + 15) / 16;
     const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, b = rest / blocks, row = rest % blocks * 16 + (threadIdx.x >> 4);
     const Sequence seq = sequence_of(a, b);
     if (row >= seq.n * w.group) return;
     const int i = row / w.group, used = (visible(a, seq, i) + w.chunk - 1) / w.chunk;
     const float *const from = w.partials + partial_row(w, b, head, row, 0) * kPartial<D>;
+    float *const mine = factors[threadIdx.x >> 4];
     float top = kNone, total = 0.0f, x[C];
-    for (int s = 0; s < used; ++s) top = fmaxf(top, from[(size_t)s * kPartial<D> + D]);
+    for (int s = lane; s < used; s += 16) top = fmaxf(top, from[(size_t)s * kPartial<D> + D]);
+    top = max_over_16_lanes(top);
+    for (int s = lane; s < used; s += 16) {
+        const float2 p = *reinterpret_cast<const float2 *>(from + (size_t)s * kPartial<D> + D);
+        mine[s] = __builtin_amdgcn_exp2f(p.x - top);
+        total = fmaf(mine[s], p.y, total);
+    }
+    lanes_exchange_fence();
+    total = dpp_add_step<0xB1>(total);
+    total = dpp_add_step<0x4E>(total);
+    total = dpp_add_step<0x141>(total);
+    total = dpp_add_step<0x140>(total);
 #pragma unroll
     for (int c = 0; c < C; ++c) x[c] = 0.0f;
+#pragma unroll 4
     for (int s = 0; s < used; ++s) {
-        const float *const p = from + (size_t)s * kPartial<D>;
-        const float f = __builtin_amdgcn_exp2f(p[D] - top);
-        total = fmaf(f, p[D + 1], total);
+        const float *const p = from + (size_t)s * kPartial<D> + first;
+        const float f = mine[s];
 #pragma unroll
-        for (int c = 0; c < C; ++c) x[c] = fmaf(f, p[first + c], x[c]);
+        for (int c = 0; c < C; c += 2) {
+            const float2 v = *reinterpret_cast<const float2 *>(p + c);
+            x[c] = fmaf(f, v.x, x[c]);
+            x[c + 1] = fmaf(f, v.y, x[c + 1]);
+        }
     }
     const float f = total != 0.0f ? 1.0f / total : 0.0f;
     uint32_t *const to = reinterpret_cast<uint32_t *>(a.out + ((long long)(seq.q0 + i) * a.q_heads + head * w.group + row - i * w.group) * D + first);
@@ -555,17 +632,26 @@ __global__ __launch_bounds__(256) void attention_join_kernel(Cut w)
     for (int c = 0; c < C; c += 2) to[c / 2] = pack_bf16x2(x[c] * f, x[c + 1] * f);
 }
 
+#define FEW(d, nq, waves) {reinterpret_cast<const void *>(attention_few_rows_kernel<d, nq, waves>), waves * 128 * d}
+const LdsKernel lds_kernels_list[] = {FEW(64, 1, 4), FEW(64, 1, 8), FEW(64, 2, 4), FEW(64, 2, 8), FEW(128, 1, 4), FEW(128, 1, 8), FEW(128, 2, 4), FEW(128, 2, 8)};
+#undef FEW
+const LdsKernels lds_kernels(lds_kernels_list);
+
 template <int D>
 hipError_t launch(const Attention &a, hipStream_t stream)
 {
     const int group = a.q_heads / a.kv_heads;
-    const AttentionPlan p = attention_plan(a.seqs, a.max_q, a.max_kv, a.q_heads, a.kv_heads, D);
+    const AttentionPlan p = attention_plan(a.seqs, a.max_q, a.max_kv, a.q_heads, a.kv_heads, D, a.causal);
     const Cut w{a, group, p.chunk, p.splits, p.tiles, a.scale == 0.0f ? 1.0f : __builtin_fabsf(a.scale) * kLog2e, a.scale < 0.0f ? 0x80008000u : 0u, a.scale == 0.0f ? 0u : 0xffffffffu,
                 static_cast<float *>(a.workspace)};
     const dim3 grid((unsigned)a.seqs * a.kv_heads * p.tiles * p.splits);
-    if (p.few) attention_few_rows_kernel<D><<<grid, 256, 0, stream>>>(w);
+    hipError_t e = p.few ? prepare_device() : hipSuccess;
+    if (e != hipSuccess) return e;
+    const bool one = (long long)a.max_q * group <= 16;
+    if (p.few && p.waves == 8) (one ? attention_few_rows_kernel<D, 1, 8> : attention_few_rows_kernel<D, 2, 8>)<<<grid, 512, 8 * 128 * D, stream>>>(w);
+    else if (p.few) (one ? attention_few_rows_kernel<D, 1, 4> : attention_few_rows_kernel<D, 2, 4>)<<<grid, 256, 4 * 128 * D, stream>>>(w);
     else attention_own_rows_kernel<D><<<grid, 256, 0, stream>>>(w);
-    const hipError_t e = hipGetLastError();
+    e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
     attention_join_kernel<D><<<dim3((unsigned)a.seqs * a.kv_heads * ((a.max_q * group + 15) / 16)), 256, 0, stream>>>(w);
     return hipGetLastError();

@@ -4,45 +4,70 @@
 
 namespace qvggt {
 
-constexpr int kAttentionTile = 32;                  // rows of a wave: query tokens times the query heads that share a key head
-constexpr int kAttentionWaves = 4;
+constexpr int kAttentionTile = 32;                  // rows of a wave, query tokens times the query heads that share a key head, where a block has four times as many
+constexpr int kAttentionFewRows = 32;               // rows of a key head up to which a block's waves share them
 constexpr long long kAttentionMostBlocks = 1 << 23; // of a launch
 constexpr int kAttentionKeys = 128;                 // parts of the keys are multiples of it
+constexpr int kAttentionMostParts = 256;            // of a sequence's keys
 
 constexpr long long attention_div_up(long long a, long long b) { return (a + b - 1) / b; }
 
 struct AttentionPlan {
     bool few;                   // the waves of a block share the rows and have keys of their own
+    int waves;                  // of a block
     int tiles, chunk, splits;   // blocks of rows of a head; keys of a part, and how many of those the longest sequence has
     size_t bytes;               // of workspace
 };
-inline AttentionPlan attention_plan(int seqs, int max_q, int max_kv, int q_heads, int kv_heads, int d)
+inline AttentionPlan attention_plan(int seqs, int max_q, int max_kv, int q_heads, int kv_heads, int d, int causal)
 {
     AttentionPlan p;
     const long long rows = (long long)max_q * (q_heads / kv_heads), pairs = (long long)seqs * kv_heads;
-    p.few = rows <= kAttentionTile;
-    p.tiles = (int)(p.few ? 1 : attention_div_up(rows, kAttentionTile * kAttentionWaves));
-    const double resident = 256 * (p.few ? 2 : d == 64 ? 3 : 2), blocks = (double)p.tiles * pairs;      // blocks that the chip holds at a time
-    // Parts: turns of the resident blocks times a part's keys and what a block costs besides, and the partial sums to memory and back; in units of the time that a block takes for a key
-    const double start = p.few ? 700.0 : 250.0;
+    p.few = rows <= kAttentionFewRows;
+    p.waves = 4;
+    p.tiles = (int)(p.few ? 1 : attention_div_up(rows, kAttentionTile * 4));
+    const double blocks = (double)p.tiles * pairs;
+    const double most = 256.0 * (p.few ? d == 64 ? 4 : 2 : d == 64 ? 3 : 2);        // blocks that the chip holds at a time
+    // Into how many parts the keys are cut, by what each number would cost, in microseconds: turns of the blocks that the chip holds, times a part's keys, and the partial sums to memory and
+    // back.  Sequences are taken to have half of the keys that are stated where there are several, and causal rows to see the mean of what the first and the last one see.
+    const double seen = (seqs > 1 ? 0.55 : 1.0) * max_kv, reach = !causal ? seen : max_q < max_kv ? seen - 0.5 * max_q * (seen / max_kv) : 0.5 * seen;
     double best = 0.0;
     p.splits = 0;
     p.chunk = kAttentionKeys;
-    for (int n = 1; n <= 256 && (n == 1 || (attention_div_up(max_kv, n) >= kAttentionKeys && blocks * n < 1 << 20)); ++n) {
-        const int chunk = (int)(attention_div_up(attention_div_up(max_kv, n), kAttentionKeys) * kAttentionKeys);
-        double turns = blocks * n / resident;
-        turns = turns > 2.0 ? turns + 0.5 : (double)(int)(turns + 0.999);
-        const double join = n == 1 ? 0.0 : (p.few ? 1200.0 : 200.0) + (double)pairs * rows * n * (d + 2) * 8 / 4.5e6 / 0.02;
-        const double cost = turns * (chunk + start) + join;
+    for (int i = 2, n = 1; n <= kAttentionMostParts && (n == 1 || (attention_div_up(max_kv, n) >= kAttentionKeys && blocks * n < 1 << 20)); ++i) {       // 1, 2, 3, 4, 6, 8, 12, 16, ...
+        const long long chunk = attention_div_up(attention_div_up(max_kv, n), kAttentionKeys) * kAttentionKeys;
+        const double live = n == 1 ? blocks : blocks * (reach / chunk + 0.5), at_once = live < most ? live : most, turns = live / at_once;
+        double part;
+        if (p.few) {
+            // the blocks of a CU stream 52 GB/s (64 channels: 37), all of them 5.8 TB/s
+            const double keys = n == 1 && turns > 1.0 ? reach : (double)chunk;
+            const double alone = keys * (d == 64 ? 0.0069 : 0.0098) * (at_once > 256.0 ? 2 : 1), all = at_once * keys * 4 * d / 5.8e6;
+            part = (alone > all ? alone + 0.15 * all : all + 0.15 * alone) + 2.5;
+        } else {
+            // 64 keys: one block on a CU 0.93 us (64 channels: 0.81), two 1.63, three 1.3
+            const double keys = n == 1 && turns > 1.0 ? reach : (double)chunk;
+            part = keys * (d == 64 ? at_once <= 256.0 ? 0.0126 : at_once <= 512.0 ? 0.0150 : 0.0203 : at_once <= 256.0 ? 0.0146 : 0.0255) + 4.0;
+        }
+        const double join = n == 1 ? 0.0 : (p.few ? 6.0 + 0.08 * n : 5.0) + live / blocks * (double)pairs * rows * (d + 2) * 8 / 4.5e6;
+        const double cost = (turns > 1.0 ? turns + 0.4 : 1.0) * part + join;
         if (p.splits == 0 || cost < best) {
             best = cost;
-            p.chunk = chunk < kAttentionKeys ? kAttentionKeys : chunk;
+            p.chunk = (int)(chunk < kAttentionKeys ? kAttentionKeys : chunk);
             p.splits = n;
         }
+        n = n == 1 ? 2 : i % 2 ? n / 2 * 3 : n / 3 * 4;
     }
     p.splits = max_kv > 0 ? (int)attention_div_up(max_kv, p.chunk) : 1;
+    // Whole sequences of few rows, a CU for each: eight waves (one row of 32 heads on 8, 601 keys: 8.1 us, 9.5 with four; as fast where keys are cut or blocks share CUs)
+    if (p.few && p.splits == 1 && blocks <= 256.0) p.waves = 8;
     p.bytes = p.splits == 1 ? 0 : (size_t)pairs * rows * p.splits * (d + 2) * sizeof(float);
     return p;
+}
+
+// What either kind of call needs (a caller asks for its sizes, not for the mask).
+inline size_t attention_workspace(int seqs, int max_q, int max_kv, int q_heads, int kv_heads, int d)
+{
+    const size_t whole = attention_plan(seqs, max_q, max_kv, q_heads, kv_heads, d, 0).bytes, causal = attention_plan(seqs, max_q, max_kv, q_heads, kv_heads, d, 1).bytes;
+    return whole > causal ? whole : causal;
 }
 
 }  // namespace qvggt

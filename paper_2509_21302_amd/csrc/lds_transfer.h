@@ -20,6 +20,11 @@ __device__ inline void dma16(uint32_t lane_off, const void *base, uint32_t lds_b
 {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 offset:%3" ::"v"(lane_off), "s"(base), "s"(lds_base), "n"(OFF) : "memory", "m0");
 }
+// the same of what nobody reads again: past the caches
+__device__ inline void dma16_once(uint32_t lane_off, const void *base, uint32_t lds_base)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(lane_off), "s"(base), "s"(lds_base) : "memory", "m0");
+}
 // the same to lds_base + AT, the global address as it is
 template <int AT>
 __device__ inline void dma16_at(uint32_t lane_off, const void *base, uint32_t lds_base)

@@ -72,8 +72,10 @@ PLAN = r"""
 #include <cstdlib>
 int main(int, char **v)
 {
-    const auto p = qvggt::attention_plan(atoi(v[1]), atoi(v[2]), atoi(v[3]), atoi(v[4]), atoi(v[5]), atoi(v[6]));
-    std::printf("%d %d %d %d %zu\n", p.few, p.tiles, p.chunk, p.splits, p.bytes);
+    for (int causal = 0; causal < 2; ++causal) {
+        const auto p = qvggt::attention_plan(atoi(v[1]), atoi(v[2]), atoi(v[3]), atoi(v[4]), atoi(v[5]), atoi(v[6]), causal);
+        std::printf("%d %d %d %d %d %zu %zu\n", p.few, p.waves, p.tiles, p.chunk, p.splits, p.bytes, qvggt::attention_workspace(atoi(v[1]), atoi(v[2]), atoi(v[3]), atoi(v[4]), atoi(v[5]), atoi(v[6])));
+    }
 }
 """
 
@@ -87,11 +89,12 @@ def test_plan_covers_all_rows_and_keys(tmp_path):
     for seqs, max_q, max_kv, (heads, kv), d in itertools.product((1, 7, 64, 65535), (1, 9, 129, 12289), (0, 1, 127, 1000, 131071, 1 << 30), ((1, 1), (32, 8), (64, 1), (16, 16)), (64, 128)):
         if seqs * kv * -(-max_q * (heads // kv) // 32) > 1 << 23:
             continue
-        few, tiles, chunk, splits, size = map(int, subprocess.run([exe, *map(str, (seqs, max_q, max_kv, heads, kv, d))], check=True, capture_output=True, text=True).stdout.split())
-        rows = max_q * (heads // kv)
-        assert tiles * (32 if few else 128) >= rows and (few == 0 or rows <= 32) and chunk % 64 == 0 and chunk > 0 and splits >= 1
-        assert chunk * splits >= max_kv and (splits == 1 or chunk * (splits - 1) < max_kv)
-        assert size == (0 if splits == 1 else seqs * kv * rows * splits * (d + 2) * 4) and seqs * kv * tiles * splits < 1 << 31
+        for line in subprocess.run([exe, *map(str, (seqs, max_q, max_kv, heads, kv, d))], check=True, capture_output=True, text=True).stdout.splitlines():
+            few, waves, tiles, chunk, splits, size, whole = map(int, line.split())
+            rows = max_q * (heads // kv)
+            assert tiles * (32 if few else 128) >= rows and (few == 0 or rows <= 32) and waves in ((4, 8) if few else (4,)) and chunk % 64 == 0 and chunk > 0 and 1 <= splits <= 256
+            assert chunk * splits >= max_kv and (splits == 1 or chunk * (splits - 1) < max_kv)
+            assert size == (0 if splits == 1 else seqs * kv * rows * splits * (d + 2) * 4) and whole >= size and seqs * kv * tiles * splits < 1 << 31
 
 
 def test_binding_refuses():
