@@ -36,19 +36,20 @@ inline AttentionPlan attention_plan(int seqs, int max_q, int max_kv, int q_heads
     for (int i = 2, n = 1; n <= kAttentionMostParts && (n == 1 || (attention_div_up(max_kv, n) >= kAttentionKeys && blocks * n < 1 << 20)); ++i) {       // 1, 2, 3, 4, 6, 8, 12, 16, ...
         const long long chunk = attention_div_up(attention_div_up(max_kv, n), kAttentionKeys) * kAttentionKeys;
         const double live = n == 1 ? blocks : blocks * (reach / chunk + 0.5), at_once = live < most ? live : most, turns = live / at_once;
-        double part;
+        double cost;
         if (p.few) {
-            // the blocks of a CU stream 52 GB/s (64 channels: 37), all of them 5.8 TB/s
+            // The blocks of a CU stream 52 GB/s (64 channels: 37), all of them 5.8 TB/s; the last turn is half empty
             const double keys = n == 1 && turns > 1.0 ? reach : (double)chunk;
             const double alone = keys * (d == 64 ? 0.0069 : 0.0098) * (at_once > 256.0 ? 2 : 1), all = at_once * keys * 4 * d / 5.8e6;
-            part = (alone > all ? alone + 0.15 * all : all + 0.15 * alone) + 2.5;
+            cost = (turns > 1.0 ? turns + 0.4 : 1.0) * ((alone > all ? alone + 0.15 * all : all + 0.15 * alone) + 2.5);
+            if (n > 1) cost += 6.0 + 0.08 * n + live * rows * (d + 2) * 8 / 4.5e6;
         } else {
-            // 64 keys: one block on a CU 0.93 us (64 channels: 0.81), two 1.63, three 1.3
-            const double keys = n == 1 && turns > 1.0 ? reach : (double)chunk;
-            part = keys * (d == 64 ? at_once <= 256.0 ? 0.0126 : at_once <= 512.0 ? 0.0150 : 0.0203 : at_once <= 256.0 ? 0.0146 : 0.0255) + 4.0;
+            // 64 keys: one block on a CU 0.93 us (64 channels: 0.81), two 1.63 (0.96), three 1.3.  Blocks that see different numbers of keys leave little of the last turn empty
+            const double key = d == 64 ? at_once <= 256.0 ? 0.0126 : at_once <= 512.0 ? 0.0150 : 0.0203 : at_once <= 256.0 ? 0.0146 : 0.0255;
+            const double all = blocks * reach * key / at_once + 0.2 * chunk * key;
+            cost = 4.0 * turns + (turns > 1.0 && all > chunk * key ? all : causal && n == 1 && at_once > 256.0 ? 0.8 * chunk * key : chunk * key);
+            if (n > 1) cost += 8.0 + live / p.tiles * rows * (d + 2) * 8 / 7e6;
         }
-        const double join = n == 1 ? 0.0 : (p.few ? 6.0 + 0.08 * n : 5.0) + live / blocks * (double)pairs * rows * (d + 2) * 8 / 4.5e6;
-        const double cost = (turns > 1.0 ? turns + 0.4 : 1.0) * part + join;
         if (p.splits == 0 || cost < best) {
             best = cost;
             p.chunk = (int)(chunk < kAttentionKeys ? kAttentionKeys : chunk);
