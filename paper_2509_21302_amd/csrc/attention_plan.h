@@ -33,7 +33,9 @@ inline AttentionPlan attention_plan(int seqs, int max_q, int max_kv, int q_heads
     double best = 0.0;
     p.splits = 0;
     p.chunk = kAttentionKeys;
-    for (int i = 2, n = 1; n <= kAttentionMostParts && (n == 1 || (attention_div_up(max_kv, n) >= kAttentionKeys && blocks * n < 1 << 20)); ++i) {       // 1, 2, 3, 4, 6, 8, 12, 16, ...
+    // (many rows whose blocks fill the chip are not cut: two prompts of 2048 tokens, 16 heads x 128, 46 us whole, 52 in two parts)
+    const int parts = !p.few && blocks >= 0.9 * most ? 1 : kAttentionMostParts;
+    for (int i = 2, n = 1; n <= parts && (n == 1 || (attention_div_up(max_kv, n) >= kAttentionKeys && blocks * n < 1 << 20)); ++i) {       // 1, 2, 3, 4, 6, 8, 12, 16, ...
         const long long chunk = attention_div_up(attention_div_up(max_kv, n), kAttentionKeys) * kAttentionKeys;
         const double live = n == 1 ? blocks : blocks * (reach / chunk + 0.5), at_once = live < most ? live : most, turns = live / at_once;
         double cost;
