@@ -9,8 +9,9 @@
 // Keys and values go straight from memory into LDS, 16 bytes a lane, rows as they are.  A row's 16-byte pieces change places by its number (the source address does that), so that reads
 // of rows of keys, and of a few rows of values, touch every bank as often as any other.
 //
-// The running maximum of a row is raised when one of its scores exceeds it by more than 2^8 in weight: weights are at most 2^8 then, and sums are multiplied by a factor in few steps.  Weights
-// are rounded to bf16 (to nearest), for the product and for the sum that it is divided by alike.  A row starts from a maximum of -3e38, so that rows that see nothing end with a sum of 0.
+// The running maximum of a row is raised when scores exceed it by much: weights are at most 2^8 or 2^12 then, which costs bf16 and fp32 nothing, and sums are multiplied by a factor in few steps.
+// In the steps that all rows of a block see it is not even looked for: the sum of a step's weights says whether one of them is too large, and only then are they made again (what that saves is 12 %
+// of the vector instructions: 13740 rows on as many keys, 16 heads x 64, 809 us for 856; 8192 on 8192, 16 x 128, 485 for 501).  Weights are rounded to bf16 (to nearest), for the product and for the sum that it is divided by alike.  A row starts from a maximum of -3e38, so that rows that see nothing end with a sum of 0.
 #include <type_traits>
 
 #include "attention.h"
@@ -33,7 +34,7 @@ union Operand {
 };
 
 constexpr float kNone = -3.0e38f, kLog2e = 1.4426950408889634f;
-constexpr float kSlack = 8.0f;
+constexpr float kSlack = 8.0f, kMostWeights = 4096.0f;       // log2 of a weight; a lane's weights of a step
 
 struct Cut {
     Attention a;
@@ -165,34 +166,65 @@ struct Wave {
             top[n] = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
         }
     }
-    // ... and the maxima raised to them where that is called for.
-    __device__ void raise(const float (&m)[NQ], float scale2)
+    // ... and the maxima raised to them where that is called for.  Of every row for itself: its result does not depend on the wave's other rows.
+    __device__ void raise(const float (&m)[NQ], const bool (&higher)[NQ], float scale2)
     {
-        bool higher = false;
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) higher |= (m[n] - top[n]) * scale2 > kSlack;
-        if (__builtin_amdgcn_ballot_w64(higher)) {
+        for (int n = 0; n < NQ; ++n) {
+            const float next = higher[n] ? fmaxf(top[n], m[n]) : top[n], f = __builtin_amdgcn_exp2f((top[n] - next) * scale2);
+            top[n] = next;
+            sum[n] *= f;
 #pragma unroll
-            for (int n = 0; n < NQ; ++n) {
-                const float next = fmaxf(top[n], m[n]), f = __builtin_amdgcn_exp2f((top[n] - next) * scale2);
-                top[n] = next;
-                sum[n] *= f;
+            for (int c = 0; c < kTiles; ++c)
 #pragma unroll
-                for (int c = 0; c < kTiles; ++c)
-#pragma unroll
-                    for (int i = 0; i < kSums; ++i) o[c][n][i] *= f;
-            }
+                for (int i = 0; i < kSums; ++i) o[c][n][i] *= f;
         }
     }
-    // Weights of NK tiles of keys, as operands.
+    // Where scores exceed a maximum by kSlack.
     template <int NK>
-    __device__ void weights(const Sums (&x)[NK][NQ], float scale2, Operand (&p)[NK * M / kKeys][NQ])
+    __device__ void raise_to(const Sums (&x)[NK][NQ], float scale2)
+    {
+        float m[NQ];
+        bool higher[NQ], any = false;
+        largest(x, m);
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) any |= higher[n] = (m[n] - top[n]) * scale2 > kSlack;
+        if (__builtin_amdgcn_ballot_w64(any)) raise(m, higher, scale2);
+    }
+    // Where a row's weights of a step, of which each of its lanes has a sum, are too large (or no numbers); whether there is such a row.
+    template <int NK>
+    __device__ bool raise_by(const float (&s)[NQ], const Sums (&x)[NK][NQ], float scale2)
+    {
+        bool any = false;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) any |= !(s[n] <= kMostWeights);
+        if (!__builtin_amdgcn_ballot_w64(any)) return false;
+        float m[NQ];
+        bool higher[NQ];
+        largest(x, m);
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            uint32_t mine = !(s[n] <= kMostWeights);
+            if (M == 16) {
+                const auto r = __builtin_amdgcn_permlane16_swap(mine, mine, false, false);
+                mine = r[0] | r[1];
+            }
+            const auto r = __builtin_amdgcn_permlane32_swap(mine, mine, false, false);
+            higher[n] = (r[0] | r[1]) != 0;
+        }
+        raise(m, higher, scale2);
+        return true;
+    }
+    // Weights of NK tiles of keys, as operands, and the lane's sums of them.
+    template <int NK>
+    __device__ void weights(const Sums (&x)[NK][NQ], float scale2, Operand (&p)[NK * M / kKeys][NQ], float (&s)[NQ])
     {
         bf16x2 one;
         one[0] = one[1] = (__bf16)1.0f;
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
             const float off = top[n] * scale2;
+            s[n] = 0.0f;
 #pragma unroll
             for (int k = 0; k < NK; ++k)
 #pragma unroll
@@ -200,7 +232,7 @@ struct Wave {
                     const float a = __builtin_amdgcn_exp2f(fmaf(x[k][n][i], scale2, -off)), b = __builtin_amdgcn_exp2f(fmaf(x[k][n][i + 1], scale2, -off));
                     const uint32_t both = pack_bf16x2(a, b);
                     p[(k * kSums + i) / 8][n].w[(k * kSums + i) % 8 / 2] = both;
-                    sum[n] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, both), one, sum[n], false);
+                    s[n] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, both), one, s[n], false);
                 }
         }
     }
@@ -300,24 +332,27 @@ __device__ inline size_t partial_row(const Cut &w, int b, int head, int row, int
     return (((size_t)b * w.a.kv_heads + head) * ((size_t)w.a.max_q * w.group) + row) * w.splits + split;
 }
 
-// The order in which a step's instructions are issued: vector instructions and LDS reads between the products, evenly (13740 rows on as many keys, 64 channels: 871 us, 898 in the compiler's own order;
-// a prompt of 11003, 128 channels: 911 and 918).
+// The order in which a step's instructions are issued: vector instructions and LDS reads between the products, evenly (13740 rows on as many keys, 16 heads x 64: 809 us for 826 in the compiler's
+// order; 8192 on 8192, 16 x 128: 485 and 521).
 template <int D>
-__device__ inline void pace()
+__device__ inline void pace_scores()
 {
-    constexpr int kProducts = D / 8, kBetween = 512 / D;
-    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);              // reads of keys ahead; then a product, vector instructions, a read
 #pragma unroll
-    for (int i = 0; i < kProducts; ++i) {                   // scores: a product, vector instructions, a read of keys
+    for (int i = 0; i < D / 8; ++i) {
         __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x2, kBetween, 0);
+        __builtin_amdgcn_sched_group_barrier(0x2, D == 128 ? 5 : 8, 0);
         __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
+}
+template <int D>
+__device__ inline void pace_values()
+{
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
-    for (int i = 0; i < kProducts; ++i) {                   // results: two reads of values, a product, vector instructions
-        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    for (int i = 0; i < D / 8; ++i) {
         __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x2, kBetween, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
 }
@@ -386,14 +421,13 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attention_own_rows_kerne
     }
     r.take(w);
     if (steps > 0) {
-        // While a step's weights are made the next one's scores are multiplied, and its maximum is looked for while this one's values are: keys are a step ahead of values
+        // While a step's weights are made the next one's scores are multiplied: keys are a step ahead of values
         float16v x[2][1], y[2][1];
         Operand p[4][1];
         arrived();
         r.scores(keys, x);
         if (steps > 1) bring_keys(1, 1);
-        float m[1];
-        r.largest(x, m);
+        float s[1];
         arrived();
         // Steps that every row of the block sees, two at a time; behind each of them there is another
         const int plain = min(max(full - t0, 0) / kKeys, steps - 1) & ~1;
@@ -402,14 +436,15 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attention_own_rows_kerne
             constexpr int kHere = decltype(parity)::value, kNext = kHere ^ 1;
             if (step + 2 < steps) bring_keys(step + 2, kHere);
             bring_values(step + 1, kNext);
-            r.raise(m, w.scale2);
             r.scores(keys + kNext * kTile, y);
-            r.weights(x, w.scale2, p);
+            r.weights(x, w.scale2, p, s);
+            pace_scores<D>();
+            if (r.raise_by(s, x, w.scale2)) r.weights(x, w.scale2, p, s);
+            r.sum[0] += s[0];
 #pragma unroll
             for (int i = 0; i < 4; ++i) r.add(values + kHere * kTile + 16 * i * R::kBytes, p[i]);
-            r.largest(y, m);
+            pace_values<D>();
             ++step;
-            pace<D>();
             arrived();
         };
         while (step < plain) {
@@ -429,11 +464,11 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attention_own_rows_kerne
             bool bad = false;
             if (t + kKeys > full) {
                 r.hide(x, t);
-                r.largest(x, m);
                 bad = __syncthreads_or(find_no_numbers(mine, kTile, threadIdx.x, 256));
             }
-            r.raise(m, w.scale2);
-            r.weights(x, w.scale2, p);
+            r.raise_to(x, w.scale2);
+            r.weights(x, w.scale2, p, s);
+            r.sum[0] += s[0];
             if (bad) {
                 r.add_no_numbers(mine, t, kKeys);
                 __syncthreads();
@@ -445,7 +480,6 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attention_own_rows_kerne
             if (more) {
                 x[0][0] = y[0][0];
                 x[1][0] = y[1][0];
-                r.largest(x, m);
             }
             arrived();
         }
@@ -521,15 +555,16 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 2 : 1) void attention_few_
         lanes_exchange_fence();
         float4v x[2][NQ];
         Operand p[1][NQ];
-        float m[NQ];
+        float s[NQ];
         r.scores(keys, x);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (more) bring_keys(t + WAVES * kKeys);
         const bool masked = t + kKeys > full;
         if (masked) r.hide(x, t);
-        r.largest(x, m);
-        r.raise(m, w.scale2);
-        r.weights(x, w.scale2, p);
+        r.raise_to(x, w.scale2);
+        r.weights(x, w.scale2, p, s);
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) r.sum[n] += s[n];
         if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kEach) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         lanes_exchange_fence();
