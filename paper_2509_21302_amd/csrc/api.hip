@@ -961,8 +961,7 @@ int qvggt_heads_norm_rope(const void *Q, const void *K, int dtype, int T, long l
     if ((q_heads > 0 && (!Q || !Q_out)) || (kv_heads > 0 && (!K || !K_out)) || (rope && !positions)) return QVGGT_ERR_NULL;
     const int vector = dtype == QVGGT_F32 ? 4 : 8;            // elements of 16 bytes
     if (!aligned16(Q) || !aligned16(K) || !aligned16(Q_out) || !aligned16(K_out) || q_stride % vector != 0 || k_stride % vector != 0 || q_out_stride % vector != 0 ||
-        k_out_stride % vector != 0 || !aligned16(q_gain) || !aligned16(q_bias) || !aligned16(k_gain) || !aligned16(k_bias) || !aligned16(rope) || !aligned16(positions) ||
-        !aligned16(pair_axis))
+        k_out_stride % vector != 0 || !aligned16(q_gain) || !aligned16(q_bias) || !aligned16(k_gain) || !aligned16(k_bias) || !aligned16(rope) || !aligned4(positions))
         return QVGGT_ERR_ALIGN;
     const qvggt::HeadsNormRope a{{Q, K}, {Q_out, K_out}, {q_stride, k_stride}, {q_out_stride, k_out_stride}, {q_heads, kv_heads}, {q_gain, k_gain}, {q_bias, k_bias}, T, dtype == QVGGT_F32,
                                  norm, eps, rope, rope_rows, rope_dim, rope_pair, axes, positions, pair_axis};

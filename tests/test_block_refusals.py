@@ -38,7 +38,7 @@ NAN, INF = float("nan"), float("inf")
     ("heads", dict(dim=144), SHAPE), ("heads", dict(pair=3), SHAPE), ("heads", dict(pair=0), SHAPE), ("heads", dict(pair=128), SHAPE), ("heads", dict(rows=0), SHAPE), ("heads", dict(axes=0), SHAPE),
     ("heads", dict(axes=5), SHAPE), ("heads", dict(norm=3), ARG), ("heads", dict(norm=-1), ARG), ("heads", dict(eps=-1e-6), ARG), ("heads", dict(eps=NAN), ARG), ("heads", dict(eps=INF), ARG),
     ("heads", dict(Q=None), NULL), ("heads", dict(K=None), NULL), ("heads", dict(qo=None), NULL), ("heads", dict(ko=None), NULL), ("heads", dict(at=None), NULL), ("heads", dict(Q=P + 8), ALIGN),
-    ("heads", dict(qs=6140), ALIGN), ("heads", dict(ks=6142, dtype=1), ALIGN), ("heads", dict(qos=4100), ALIGN), ("heads", dict(kg=P + 4), ALIGN), ("heads", dict(lanes=P + 1), ALIGN),
+    ("heads", dict(qs=6140), ALIGN), ("heads", dict(ks=6142, dtype=1), ALIGN), ("heads", dict(qos=4100), ALIGN), ("heads", dict(kg=P + 4), ALIGN), ("heads", dict(at=P + 2), ALIGN),
     ("heads", dict(rope=P + 8), ALIGN), ("heads", dict(T=0, Q=None, K=None), OK), ("heads", dict(heads=0, kv_heads=0, Q=None), OK),
     ("attention", dict(dtype=1), DTYPE), ("attention", dict(T=-1), SHAPE), ("attention", dict(S=-1), SHAPE), ("attention", dict(S=0), SHAPE), ("attention", dict(d=96), SHAPE),
     ("attention", dict(heads=30), SHAPE), ("attention", dict(heads=4), SHAPE), ("attention", dict(kv_heads=0), SHAPE), ("attention", dict(seqs=65536), SHAPE), ("attention", dict(max_q=-1), SHAPE),

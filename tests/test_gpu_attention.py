@@ -222,3 +222,46 @@ def test_another_stream_and_a_captured_call_with_other_lengths():
         graph.replay()
         assert torch.equal(out, eager)
         near(out, *O.attention(Q, K, V, 0.1, True, [(1, n) for n in now], [0, 900, 1800, 2700]))
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_random_batches(seed):
+    """Sequences of any lengths, groups of any size, buffers and packed rows, as one call."""
+    import random
+    rng = random.Random(seed)
+    d, group, kv_heads, causal = rng.choice((64, 128)), rng.choice((1, 2, 3, 5, 7, 8, 12)), rng.choice((1, 2, 3, 8)), rng.random() < 0.6
+    seqs, top_q, top_kv = rng.choice((1, 2, 5, 9)), rng.choice((1, 1, 3, 30, 200)), rng.choice((1, 40, 300, 2000))
+    lengths = [(rng.randint(0 if i else 1, top_q), rng.randint(0 if i else 1, top_kv)) for i in range(seqs)]
+    q_lens, kv_lens = zip(*lengths)
+    T, slack = sum(q_lens), rng.randint(0, 5)
+    capacity = max(kv_lens) + slack
+    packed = rng.random() < 0.5
+    first = starts_of(kv_lens) if packed else [i * capacity for i in range(seqs)]
+    S = first[-1] if packed else seqs * capacity
+    Q, K, V = inputs(T, S, group * kv_heads, kv_heads, d, seed, rng.choice((0.3, 1.5, 6.0)))
+    got = attend(Q, K, V, 0.125, causal, whole(starts_of(q_lens)), whole(first), None if packed else whole(kv_lens), max(q_lens) + rng.randint(0, 3), max(kv_lens) + rng.randint(0, 3))
+    near(got, *O.attention(Q, K, V, 0.125, causal, lengths, first))
+
+
+def test_without_any_keys():
+    Q, K, V = inputs(40, 1, 4, 2, 64, 1)
+    for n in (1, 40):
+        got = attend(Q[:n], K[:0], V[:0], 0.1, True, whole([0, n]), whole([0, 0]), None, n, 0)
+        assert bool((got == 0).all())
+        got = attend(Q[:n], K, V, 0.1, False, whole([0, n]), whole([1]), whole([5]), n, 300)
+        assert bool((got == 0).all())
+
+
+def test_rows_past_2_to_the_31():
+    """The most sequences that a call takes; queries and results of more than 2^31 values."""
+    seqs, n, heads, d = 65535, 5, 64, 128
+    T = seqs * n
+    Q, K, V = (torch.zeros(T, heads, d, dtype=torch.bfloat16, device=DEV) for _ in range(3))
+    g = torch.Generator(DEV).manual_seed(1)
+    for t in (Q, K, V):
+        t[-4 * n:] = torch.randn(4 * n, heads, d, device=DEV, generator=g).to(torch.bfloat16)
+    at = torch.arange(seqs + 1, dtype=torch.int32, device=DEV) * n
+    out = torch.full_like(Q, 7.0)
+    q.qvggt_attention(Q, K, V, 0.1, True, at, at, None, n, n, out, workspace(T, seqs, n, n, heads, heads, d))
+    near(out[-4 * n:], *O.attention(Q[-4 * n:], K[-4 * n:], V[-4 * n:], 0.1, True, [(n, n)] * 4, [0, n, 2 * n, 3 * n]))
+    assert not bool(out[:-4 * n].any())

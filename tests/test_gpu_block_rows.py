@@ -203,3 +203,24 @@ def test_residual_offsets_past_32_bits():
     near(x[-20:], *want[0])
     near(h[-20:], *want[1])
     assert not bool(h[:-20].any())
+
+
+def test_heads_past_2_to_the_31():
+    T, heads, d = 262144, 68, 128
+    x = torch.zeros(T, heads, d, dtype=torch.bfloat16, device=DEV)
+    g = gen(10)
+    x[-3:] = torch.randn(3, heads, d, device=DEV, generator=g).to(torch.bfloat16)
+    rope, at = table_of(64, d, g), (torch.arange(2 * T, device=DEV) % 64).int().view(2, T)
+    want = O.heads_norm_rope(x[-3:], "rms", 1e-6, None, None, rope, at[:, -3:], 64)
+    q.qvggt_heads_norm_rope(x, None, x, None, norm="rms", rope=rope, positions=at, rope_pair=64)
+    near(x[-3:], *want)
+    assert not bool(x[:-3].any())
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_random_rows(seed):
+    import random
+    rng = random.Random(seed)
+    C, M, rows = 8 * rng.choice((1, 3, 16, 17, 31, 33, 63, 65, 100, 127, 129, 200, 257, 500, 511, 513, 777, 1023)), rng.choice((1, 2, 3, 17, 64, 300)), rng.choice((1, 2, 9))
+    c = case(M, C, *(rng.choice(("bf16", "f32")) for _ in range(3)), seed, rows, rng.choice(("bf16", "f32")))
+    update(c, rng.choice(("none", "rms", "layer")), rng.choice(("none", "rms", "layer")), [n for n in FULL if rng.random() < 0.6], rng.choice((1e-6, 1e-3)))
