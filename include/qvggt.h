@@ -542,7 +542,7 @@ int qvggt_kv4_attention(const void *Q, int q_dtype, int T, long long q_stride, i
  *   behind the other).  positions: int32 [axes, T], 1 <= axes <= 4 (rows outside the table are taken as its first or last); pair_axis: uint8 [rope_dim / 2] (numbers past the last axis are taken
  *   as it).  rope, rope_dim and rope_pair as there; rope = NULL: no rotation.  Q, K, Q_out, K_out: all bf16 or all f32, token t at its stride * t elements, heads one after another (strides a
  *   multiple of 16 bytes, of outputs no less than a row).  An output may be its own input; otherwise outputs overlap neither inputs nor each other.  q_heads or kv_heads = 0: without queries, or
- *   keys.  T * (q_heads + kv_heads) at most 2^27.  positions need 4-byte alignment only, pair_axis none.
+ *   keys.  T at most 2^25, T * (q_heads + kv_heads) at most 2^27.  positions need 4-byte alignment only, pair_axis none.
  *
  * qvggt_attention:  for every sequence b, its n = q_starts[b + 1] - q_starts[b] query tokens (rows q_starts[b] .. of Q) over its len keys and values, rows kv_starts[b] .. of K and V:
  *     out[i, h, :] = sum_j softmax_j( scale * <q[i, h], k[j, h']> ) v[j, h'],     h' = h / (q_heads / kv_heads),

@@ -952,7 +952,7 @@ int qvggt_heads_norm_rope(const void *Q, const void *K, int dtype, int T, long l
 {
     if (!valid_dtype(dtype)) return QVGGT_ERR_DTYPE;
     const long long q_row = (long long)q_heads * d, k_row = (long long)kv_heads * d;
-    if (T < 0 || !qvggt::kv4_valid_head(d) || q_heads < 0 || kv_heads < 0 || q_heads > 65535 || kv_heads > 65535 || (long long)T * (q_heads + kv_heads) > 1 << 27 || q_stride < 0 ||
+    if (T < 0 || T > 1 << 25 || !qvggt::kv4_valid_head(d) || q_heads < 0 || kv_heads < 0 || q_heads > 65535 || kv_heads > 65535 || (long long)T * (q_heads + kv_heads) > 1 << 27 || q_stride < 0 ||
         k_stride < 0 || !valid_rope(rope, rope_rows, rope_dim, rope_pair, d) || (rope && (axes < 1 || axes > 4)) ||
         (T > 1 && ((q_heads > 0 && q_out_stride < q_row) || (kv_heads > 0 && k_out_stride < k_row))))
         return QVGGT_ERR_SHAPE;

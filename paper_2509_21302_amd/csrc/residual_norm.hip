@@ -91,12 +91,12 @@ __device__ inline void add(const void *given, float (&x)[8], const float (&u)[8]
 
 // LANES = 0: a block has a row, of as many lanes as it has pieces.
 template <int LANES, int V, bool XF, bool YF, bool HF>
-__global__ __launch_bounds__(LANES ? 256 : 1024) void residual_norm_kernel(ResidualNorm a)
+__global__ __launch_bounds__(LANES ? 256 : 1024) void residual_norm_kernel(ResidualNorm a, long long row0)
 {
     constexpr int kLanes = LANES ? LANES : 64;          // (LANES = 0 has V = 1)
     __shared__ float red[16];
     const int lane = LANES ? threadIdx.x % kLanes : threadIdx.x;
-    const long long row = LANES ? (long long)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes : blockIdx.x;
+    const long long row = row0 + (LANES ? (long long)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes : blockIdx.x);
     if (row >= a.M) return;
     const size_t at = (size_t)row * a.C;
     const char *const x_row = static_cast<const char *>(a.x) + at * (XF ? 4 : 2), *const y_row = static_cast<const char *>(a.y) + at * (YF ? 4 : 2);
@@ -181,8 +181,12 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void residual_norm_kernel(Resid
 template <int LANES, int V, bool XF, bool YF, bool HF>
 hipError_t launch(const ResidualNorm &a, hipStream_t stream)
 {
-    if (LANES == 0) residual_norm_kernel<LANES, V, XF, YF, HF><<<dim3(a.M), dim3((a.C / 8 + 63) / 64 * 64), 0, stream>>>(a);
-    else residual_norm_kernel<LANES, V, XF, YF, HF><<<dim3((unsigned)(((long long)a.M * LANES + 255) / 256)), 256, 0, stream>>>(a);
+    const int block = LANES ? 256 : (a.C / 8 + 63) / 64 * 64, rows = LANES ? 256 / (LANES ? LANES : 1) : 1;       // of a block
+    const long long most = (1 << 30) / block * (long long)rows;             // of a launch, which has less than 2^32 threads
+    for (long long row0 = 0; row0 < a.M; row0 += most) {
+        const long long here = a.M - row0 < most ? a.M - row0 : most;
+        residual_norm_kernel<LANES, V, XF, YF, HF><<<dim3((unsigned)((here + rows - 1) / rows)), block, 0, stream>>>(a, row0);
+    }
     return hipGetLastError();
 }
 // Lanes by the row's length: few enough that all have work, and no more than a wave where a lane can hold its part (2048 channels: 90 us for 30000 rows, 94 with a block for each; more pieces a lane than

@@ -34,7 +34,7 @@ NAN, INF = float("nan"), float("inf")
 
 @pytest.mark.parametrize("name,other,status", [
     ("heads", dict(dtype=2), DTYPE), ("heads", dict(T=-1), SHAPE), ("heads", dict(d=96), SHAPE), ("heads", dict(heads=-1), SHAPE), ("heads", dict(kv_heads=65536), SHAPE),
-    ("heads", dict(T=1 << 22), SHAPE), ("heads", dict(qs=-8), SHAPE), ("heads", dict(ks=-8), SHAPE), ("heads", dict(qos=4088), SHAPE), ("heads", dict(kos=8), SHAPE), ("heads", dict(dim=24), SHAPE),
+    ("heads", dict(T=1 << 22), SHAPE), ("heads", dict(T=(1 << 25) + 1, heads=1, kv_heads=0), SHAPE), ("heads", dict(qs=-8), SHAPE), ("heads", dict(ks=-8), SHAPE), ("heads", dict(qos=4088), SHAPE), ("heads", dict(kos=8), SHAPE), ("heads", dict(dim=24), SHAPE),
     ("heads", dict(dim=144), SHAPE), ("heads", dict(pair=3), SHAPE), ("heads", dict(pair=0), SHAPE), ("heads", dict(pair=128), SHAPE), ("heads", dict(rows=0), SHAPE), ("heads", dict(axes=0), SHAPE),
     ("heads", dict(axes=5), SHAPE), ("heads", dict(norm=3), ARG), ("heads", dict(norm=-1), ARG), ("heads", dict(eps=-1e-6), ARG), ("heads", dict(eps=NAN), ARG), ("heads", dict(eps=INF), ARG),
     ("heads", dict(Q=None), NULL), ("heads", dict(K=None), NULL), ("heads", dict(qo=None), NULL), ("heads", dict(ko=None), NULL), ("heads", dict(at=None), NULL), ("heads", dict(Q=P + 8), ALIGN),

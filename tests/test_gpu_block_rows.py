@@ -224,3 +224,17 @@ def test_random_rows(seed):
     C, M, rows = 8 * rng.choice((1, 3, 16, 17, 31, 33, 63, 65, 100, 127, 129, 200, 257, 500, 511, 513, 777, 1023)), rng.choice((1, 2, 3, 17, 64, 300)), rng.choice((1, 2, 9))
     c = case(M, C, *(rng.choice(("bf16", "f32")) for _ in range(3)), seed, rows, rng.choice(("bf16", "f32")))
     update(c, rng.choice(("none", "rms", "layer")), rng.choice(("none", "rms", "layer")), [n for n in FULL if rng.random() < 0.6], rng.choice((1e-6, 1e-3)))
+
+
+def test_residual_rows_of_several_launches():
+    M, C = (1 << 26) + 37, 8
+    x, y = torch.zeros(M, C, dtype=torch.bfloat16, device=DEV), torch.zeros(M, C, dtype=torch.bfloat16, device=DEV)
+    g = gen(11)
+    at = slice((1 << 26) - 20, M)
+    x[at], y[at] = (torch.randn(57, C, device=DEV, generator=g).to(torch.bfloat16) for _ in range(2))
+    want = O.residual_norm(x[at], y[at], torch.bfloat16, torch.bfloat16, kind="rms")
+    h = torch.full_like(x, 7.0)
+    q.qvggt_residual_norm(x, y, x, h, norm="rms")
+    near(x[at], *want[0])
+    near(h[at], *want[1])
+    assert not bool(h[:(1 << 26) - 20].any())
