@@ -11,7 +11,8 @@
 //
 // The running maximum of a row is raised when scores exceed it by much: weights are at most 2^8 or 2^12 then, which costs bf16 and fp32 nothing, and sums are multiplied by a factor in few steps.
 // In the steps that all rows of a block see it is not even looked for: the sum of a step's weights says whether one of them is too large, and only then are they made again (what that saves is 12 %
-// of the vector instructions: 13740 rows on as many keys, 16 heads x 64, 809 us for 856; 8192 on 8192, 16 x 128, 485 for 501).  Weights are rounded to bf16 (to nearest), for the product and for the sum that it is divided by alike.  A row starts from a maximum of -3e38, so that rows that see nothing end with a sum of 0.
+// of the vector instructions: 13740 rows on as many keys, 16 heads x 64, 809 us for 856; 8192 on 8192, 16 x 128, 485 for 501).  Weights are rounded to bf16 (to nearest), for the product and for the sum
+// that it is divided by alike.  A row starts from a maximum of -3e38 over the scale (over 1 for small ones), so that rows that see nothing end with a sum of 0.
 #include <type_traits>
 
 #include "attention.h"
@@ -41,6 +42,7 @@ struct Cut {
     int group, chunk, splits, tiles;        // query heads of a key head; keys of a part; parts and tiles of rows that there may be
     float scale2;                           // |scale| log2(e); its sign, and a scale of 0, are in the queries
     uint32_t flip, keep;                    // ... as masks of pairs of them
+    float none;                             // the maximum that a row starts from: times scale2 it is a number, so that an unseen key's weight is 0 by it
     float *partials;                        // [seqs][key heads][rows][splits][D + 2]: a row's sums, maximum and weights' sum
 };
 
@@ -98,7 +100,7 @@ struct Wave {
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
             const int row = row0 + M * n + lane % M, r = min(row, rows - 1), i = r / w.group;
-            top[n] = kNone;
+            top[n] = w.none;
             sum[n] = 0.0f;
             end[n] = row < rows ? visible(w.a, s, i) : 0;
             const uint16_t *const from = w.a.q + (long long)(s.q0 + i) * w.a.q_stride + (head * w.group + r - i * w.group) * D + 8 * g;
@@ -596,7 +598,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 2 : 1) void attention_few_
     __syncthreads();
     for (int i = threadIdx.x; i < rows * kFours; i += 64 * WAVES) {
         const int row = i / kFours, c = i % kFours;
-        float top = kNone, all = 0.0f;
+        float top = w.none, all = 0.0f;
 #pragma unroll
         for (int n = 0; n < WAVES; ++n) top = fmaxf(top, tops[n][row]);
         float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -677,7 +679,8 @@ hipError_t launch(const Attention &a, hipStream_t stream)
 {
     const int group = a.q_heads / a.kv_heads;
     const AttentionPlan p = attention_plan(a.seqs, a.max_q, a.max_kv, a.q_heads, a.kv_heads, D, a.causal);
-    const Cut w{a, group, p.chunk, p.splits, p.tiles, a.scale == 0.0f ? 1.0f : __builtin_fabsf(a.scale) * kLog2e, a.scale < 0.0f ? 0x80008000u : 0u, a.scale == 0.0f ? 0u : 0xffffffffu,
+    const float scale2 = a.scale == 0.0f ? 1.0f : __builtin_fabsf(a.scale) * kLog2e;
+    const Cut w{a, group, p.chunk, p.splits, p.tiles, scale2, a.scale < 0.0f ? 0x80008000u : 0u, a.scale == 0.0f ? 0u : 0xffffffffu, scale2 > 1.0f ? kNone / scale2 : kNone,
                 static_cast<float *>(a.workspace)};
     const dim3 grid((unsigned)a.seqs * a.kv_heads * p.tiles * p.splits);
     hipError_t e = p.few ? prepare_device() : hipSuccess;

@@ -89,6 +89,19 @@ def test_scales(d, n, m, group, scale):
 
 
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n,m,group", [(8, 33, 4), (4, 70, 1), (30, 98, 1), (40, 20, 1), (300, 40, 2), (20, 5, 1), (61, 3010, 4)])
+@pytest.mark.parametrize("scale", [0.79, 1.0, -4.0, 1e4])
+def test_rows_that_see_nothing_of_a_step_at_large_scales(d, n, m, group, scale):
+    """A starting maximum times the scale has no place in fp32; rows without keys, and waves whose keys a row does not see, add zeros all the same."""
+    Q, K, V = inputs(n, m, 2 * group, 2, d, n + m)
+    if abs(scale) > 100:
+        Q[:], K[:] = Q / 128, K / 128
+    got = attend(Q, K, V, scale, True, whole([0, n]), whole([0, m]), None, n, m)
+    assert bool(torch.isfinite(got.float()).all())
+    near(got, *O.attention(Q, K, V, scale, True, [(n, m)], [0]))
+
+
+@pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("n,m", [(1, 900), (130, 130), (40, 2500), (700, 700)])
 def test_scores_rise_along_the_keys(d, n, m):
     """Every step has a new maximum, by much and by little; and falls: all later weights vanish."""
