@@ -541,13 +541,15 @@ int qvggt_kv4_attention(const void *Q, int q_dtype, int T, long long q_stride, i
  *   of a token is the one at column p of row positions[axis][token] of the table, axis = pair_axis[p], or p * axes / (rope_dim / 2) where pair_axis is NULL (sections of equal length, one
  *   behind the other).  positions: int32 [axes, T], 1 <= axes <= 4 (rows outside the table are taken as its first or last); pair_axis: uint8 [rope_dim / 2] (numbers past the last axis are taken
  *   as it).  rope, rope_dim and rope_pair as there; rope = NULL: no rotation.  Q, K, Q_out, K_out: all bf16 or all f32, token t at its stride * t elements, heads one after another (strides a
- *   multiple of 16 bytes, of outputs no less than a row).  An output may be its own input; otherwise outputs overlap neither inputs nor each other.  q_heads or kv_heads = 0: without queries, or
+ *   multiple of 16 bytes, of outputs no less than a row).  An output may be its own input, at the same stride; otherwise outputs overlap neither inputs nor each other (QVGGT_ERR_ARG where
+ *   they begin at one address).  q_heads or kv_heads = 0: without queries, or
  *   keys.  T at most 2^25, T * (q_heads + kv_heads) at most 2^27.  positions need 4-byte alignment only, pair_axis none.
  *
  * qvggt_attention:  for every sequence b, its n = q_starts[b + 1] - q_starts[b] query tokens (rows q_starts[b] .. of Q) over its len keys and values, rows kv_starts[b] .. of K and V:
  *     out[i, h, :] = sum_j softmax_j( scale * <q[i, h], k[j, h']> ) v[j, h'],     h' = h / (q_heads / kv_heads),
  *   j over the keys 0 .. len - n + i with causal = 1 (the queries are the sequence's last n tokens), 0 .. len - 1 with causal = 0.  A query that sees no key gives zeros.
- *   dtype: QVGGT_BF16, of Q, K, V and out.  Q [T, q_heads, d], K and V [S, kv_heads, d] at their strides (elements, multiples of 8; k_stride and v_stride below 2^24); d = 64 or 128; q_heads a
+ *   |scale| <= 1e38.  dtype: QVGGT_BF16, of Q, K, V and out.  Q [T, q_heads, d], K and V [S, kv_heads, d] at their strides (elements, multiples of 8; k_stride and v_stride below 2^24);
+ *   d = 64 or 128; q_heads a
  *   multiple of kv_heads.  q_starts: int32 [seqs + 1], not falling.  kv_lens = NULL: kv_starts is int32 [seqs + 1] and len the difference (whole prompts: kv_starts = q_starts); otherwise
  *   kv_starts and kv_lens are int32 [seqs] (a buffer for every sequence that its tokens are added to, for example).  Starts and lengths are read on the device: a call can be captured and replayed
  *   with others.  Those that lead outside of T and S are cut.  max_q and max_kv: at least every n and len (they decide how the work is cut up; of a longer sequence the first max_q queries are

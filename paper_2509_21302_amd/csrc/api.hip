@@ -919,7 +919,7 @@ int qvggt_kv4_attention(const void *Q, int q_dtype, int T, long long q_stride, i
     if (!valid_pages(num_pages, page_tokens, kv_heads, d) || !valid_attention(T, seqs, max_q, max_kv, q_heads, kv_heads, d) || q_stride < 0 ||
         !valid_rope(rope, rope_rows, rope_dim, rope_pair, d) || table_width < 0 || max_kv > (long long)table_width * page_tokens || (max_kv > 0 && num_pages == 0))
         return QVGGT_ERR_SHAPE;
-    if (!std::isfinite(scale) || (causal != 0 && causal != 1)) return QVGGT_ERR_ARG;
+    if (!(std::fabs(scale) <= 1e38f) || (causal != 0 && causal != 1)) return QVGGT_ERR_ARG;
     if (T == 0 || seqs == 0 || max_q == 0) return QVGGT_OK;
     const size_t need = qvggt::kv4_attention_workspace_bytes(seqs, max_q, max_kv, q_heads, kv_heads, d);
     if (!Q || !q_starts || !kv_lens || !out || (rope && !positions) || (max_kv > 0 && (!cache || !page_table)) || (need > 0 && !workspace)) return QVGGT_ERR_NULL;
@@ -963,6 +963,10 @@ int qvggt_heads_norm_rope(const void *Q, const void *K, int dtype, int T, long l
     if (!aligned16(Q) || !aligned16(K) || !aligned16(Q_out) || !aligned16(K_out) || q_stride % vector != 0 || k_stride % vector != 0 || q_out_stride % vector != 0 ||
         k_out_stride % vector != 0 || !aligned16(q_gain) || !aligned16(q_bias) || !aligned16(k_gain) || !aligned16(k_bias) || !aligned16(rope) || !aligned4(positions))
         return QVGGT_ERR_ALIGN;
+    // an output that is its own input has that one's rows; heads of two kinds never have one place
+    if ((T > 1 && ((q_heads > 0 && Q == Q_out && q_stride != q_out_stride) || (kv_heads > 0 && K == K_out && k_stride != k_out_stride))) ||
+        (q_heads > 0 && kv_heads > 0 && (Q_out == K_out || Q_out == K || K_out == Q)))
+        return QVGGT_ERR_ARG;
     const qvggt::HeadsNormRope a{{Q, K}, {Q_out, K_out}, {q_stride, k_stride}, {q_out_stride, k_out_stride}, {q_heads, kv_heads}, {q_gain, k_gain}, {q_bias, k_bias}, T, dtype == QVGGT_F32,
                                  norm, eps, rope, rope_rows, rope_dim, rope_pair, axes, positions, pair_axis};
     return hip_status(qvggt::run_heads_norm_rope(a, d, static_cast<hipStream_t>(stream)));
@@ -981,7 +985,7 @@ int qvggt_attention(const void *Q, const void *K, const void *V, int dtype, int 
     if (!valid_packed(T, S, seqs, max_q, max_kv, q_heads, kv_heads, d) || q_stride < 0 || k_stride < 0 || v_stride < 0 || k_stride >= kMostStride || v_stride >= kMostStride ||
         (max_kv > 0 && S == 0))
         return QVGGT_ERR_SHAPE;
-    if (!std::isfinite(scale) || (causal != 0 && causal != 1)) return QVGGT_ERR_ARG;
+    if (!(std::fabs(scale) <= 1e38f) || (causal != 0 && causal != 1)) return QVGGT_ERR_ARG;
     if (T == 0 || seqs == 0 || max_q == 0) return QVGGT_OK;
     const size_t need = qvggt::attention_workspace(seqs, max_q, max_kv, q_heads, kv_heads, d);
     if (!Q || !q_starts || !kv_starts || !out || (max_kv > 0 && (!K || !V)) || (need > 0 && !workspace)) return QVGGT_ERR_NULL;

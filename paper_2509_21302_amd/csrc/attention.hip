@@ -58,7 +58,7 @@ __device__ inline Sequence sequence_of(const Attention &a, int b)
     s.total = min(max(a.q_starts[b + 1], s.q0), a.T) - s.q0;
     s.n = min(s.total, a.max_q);
     s.k0 = min(max(a.kv_starts[b], 0), a.S);
-    s.len = min(max(a.kv_lens != nullptr ? a.kv_lens[b] : a.kv_starts[b + 1] - s.k0, 0), a.S - s.k0);
+    s.len = min(max(a.kv_lens != nullptr ? a.kv_lens[b] : max(a.kv_starts[b + 1], 0) - s.k0, 0), a.S - s.k0);
     s.limit = min(s.len, a.max_kv);
     return s;
 }

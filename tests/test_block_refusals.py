@@ -58,6 +58,17 @@ def test_refusals(name, other, status):
     assert call(name, **other) == status
 
 
+@pytest.mark.parametrize("other", [dict(qo=P), dict(ko=2 * P), dict(qo=4 * P, ko=4 * P), dict(qo=2 * P), dict(ko=P), dict(qo=P, qos=6144, ko=2 * P)])
+def test_heads_outputs_in_a_place_that_others_have(other):
+    """Rows at another distance than the input's in its place; queries and keys in one place."""
+    assert call("heads", **dict(dict(Q=P, K=2 * P, qo=3 * P, ko=4 * P), **other)) == ARG
+
+
+@pytest.mark.parametrize("scale", [1.1e38, -3e38, -INF])
+def test_scales_that_leave_fp32(scale):
+    assert call("attention", scale=scale) == ARG
+
+
 def test_workspace():
     size = q.qvggt_attention_workspace_bytes
     need = size(1, 1, 1, 131072, 32, 8, 128)

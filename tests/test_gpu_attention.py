@@ -180,6 +180,10 @@ def test_starts_and_lengths_outside_of_the_tensors_are_cut():
     near(got, want, off)
     got = attend(Q, K, V, 0.1, False, whole([0, 50, 100]), whole([500, 30]), whole([10, -4]), 100, 120)
     assert bool((got == 0).all())
+    got = attend(Q, K, V, 0.1, False, whole([0, 50, 100]), whole([30, -(1 << 31), 1 << 30]), None, 100, 120)
+    assert bool((got[:50] == 0).all())
+    want, off = O.attention(Q[50:], K, V, 0.1, False, [(50, 120)], [0])
+    near(got[50:], want, off)
 
 
 @pytest.mark.parametrize("d,n,m", [(64, 1, 40000), (128, 2, 70000)])
