@@ -359,7 +359,10 @@ __device__ inline void pace_values()
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// ---- many rows: a wave has 32 of its own, the four waves of a block go through the same keys
+// ---- many rows: a wave has 32 of its own, the four waves of a block go through the same keys, 64 a step, two tiles of each in LDS.  Products of 32 x 32 x 16: a lane's registers hold a tile and
+// the scores of the next one, for which 16 x 16 x 32, faster out of registers alone, leave no room (8192 rows on 8192 keys, 16 heads x 128: 516 us for 493).  Bound by the board's power where sequences are
+// long: 11003 tokens, 32 heads on 8 x 128, 837 to 887 us by the board, 1.12 to 1.19 PFLOP/s at 1.6 GHz, with the matrix cores busy in 0.65 of the cycles, and 651 us on zeros; with 64 channels by vector
+// instructions as well (96 for 16 products a step: 13740 rows on as many keys, 16 heads, 765 to 805 us, 0.96 to 1.01 PFLOP/s).  A block costs some 8 us besides its steps.
 template <int D>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attention_own_rows_kernel(Cut w)
 {
@@ -417,9 +420,10 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attention_own_rows_kerne
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
     };
-    if (steps > 0) {
+    if (steps > 0) {        // two tiles of keys at once (eight chunks of 61 rows, 71 us for 73; 20 frames of 1374 tokens, 16 heads x 64, 126 for 127)
         bring_keys(0, 0);
         bring_values(0, 0);
+        if (steps > 1) bring_keys(1, 1);
     }
     r.take(w);
     if (steps > 0) {
@@ -428,9 +432,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attention_own_rows_kerne
         Operand p[4][1];
         arrived();
         r.scores(keys, x);
-        if (steps > 1) bring_keys(1, 1);
         float s[1];
-        arrived();
+        __syncthreads();
         // Steps that every row of the block sees, two at a time; behind each of them there is another
         const int plain = min(max(full - t0, 0) / kKeys, steps - 1) & ~1;
         int step = 0;
@@ -516,7 +519,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attention_own_rows_kerne
     }
 }
 
-// ---- few rows (32 at most): the waves of a block share them and go through keys of their own, 32 at a time, brought into LDS by each for itself
+// ---- few rows (32 at most): the waves of a block share them and go through keys of their own, 32 at a time, brought into LDS by each for itself.  Products of 16 x 16 x 32, of whose rows fewer are
+// nobody's.  Bound by memory: 48 rows on up to 8192 keys, 32 heads on 8 x 128, 147 us, 5.8 TB/s; a block alone on a CU brings in 52 GB/s (one row on 601 keys: 7.3 us)
 template <int D, int NQ, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 2 : 1) void attention_few_rows_kernel(Cut w)
 {
