@@ -18,7 +18,7 @@ HEADS = dict(Q=P, K=P, dtype=0, T=4, qs=6144, ks=6144, heads=32, kv_heads=8, d=1
              lanes=P, qo=P, ko=P, qos=4096, kos=1024)
 ATTEND = dict(Q=P, K=P, V=P, dtype=0, T=40, S=100, qs=6144, ks=6144, vs=6144, heads=32, kv_heads=8, d=128, scale=0.1, causal=1, starts=P, kv_starts=P, lens=None, seqs=3, max_q=20, max_kv=50,
               out=P, ws=P, size=1 << 30)
-RESIDUAL = dict(x=P, xt=0, y=2 * P, yt=0, M=10, C=1024, post=1, pg=P, pb=P, scale=P, gate=P, norm=2, g=P, b=P, ms=P, mt=P, ct=0, rows=3, cs=3072, row_of=P, eps=1e-6, xo=3 * P, h=4 * P, ht=0)
+RESIDUAL = dict(x=P, xt=0, y=2 * P, yt=0, M=10, C=1024, post=1, pg=P, pb=P, scale=P, gate=P, norm=2, g=P, b=P, ms=P, mt=P, ct=0, rows=3, cs=6144, row_of=P, eps=1e-6, xo=3 * P, h=4 * P, ht=0)
 NAMES = {"heads": (q.load_library().qvggt_heads_norm_rope, HEADS), "attention": (q.load_library().qvggt_attention, ATTEND), "residual": (q.load_library().qvggt_residual_norm, RESIDUAL)}
 
 
@@ -52,7 +52,7 @@ NAN, INF = float("nan"), float("inf")
     ("residual", dict(C=1020), SHAPE), ("residual", dict(C=8200), SHAPE), ("residual", dict(rows=0), SHAPE), ("residual", dict(cs=-8), SHAPE), ("residual", dict(row_of=None), SHAPE),
     ("residual", dict(post=3), ARG), ("residual", dict(norm=-1), ARG), ("residual", dict(eps=-1.0), ARG), ("residual", dict(eps=INF), ARG), ("residual", dict(h=3 * P), ARG),
     ("residual", dict(xo=2 * P), ARG), ("residual", dict(h=P, ht=1), ARG), ("residual", dict(h=2 * P, ht=1), ARG), ("residual", dict(x=None), NULL), ("residual", dict(x=P + 8), ALIGN),
-    ("residual", dict(gate=P + 8), ALIGN), ("residual", dict(cs=3076), ALIGN), ("residual", dict(pg=P + 4), ALIGN), ("residual", dict(row_of=P + 2), ALIGN), ("residual", dict(h=4 * P + 8), ALIGN),
+    ("residual", dict(gate=P + 8), ALIGN), ("residual", dict(cs=6148), ALIGN), ("residual", dict(pg=P + 4), ALIGN), ("residual", dict(row_of=P + 2), ALIGN), ("residual", dict(h=4 * P + 8), ALIGN),
     ("residual", dict(M=0, x=None), OK), ("residual", dict(xo=None, h=None), OK)])
 def test_refusals(name, other, status):
     assert call(name, **other) == status
