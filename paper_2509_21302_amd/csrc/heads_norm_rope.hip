@@ -2,8 +2,8 @@
 //
 // d / 8 lanes have a head, eight channels each, and a wave has heads of one token: what turns them (the token's positions, its rows of the table) is found once for all of them, one pair of channels
 // a lane, and handed out through LDS (16411 tokens of 32 + 8 heads x 128 in float32, three axes whose pairs take turns: 134 us; 164 with every lane finding all of its own).  Means and variances are two
-// passes over registers, sums between lanes by DPP, and so are the channels that a lane's own turn with.  Bound by memory: 5.0 TB/s there, 5.3 on ten frames (13740 tokens of 16 + 16 heads x 64 in
-// bf16: 21 us), read and written, where a copy reaches 4.8 to 5.0.
+// passes over registers, sums between lanes by DPP, and so are the channels that a lane's own turn with.  Bound by memory: 5.1 TB/s there, 5.6 on ten frames (13740 tokens of 16 + 16 heads x 64 in
+// bf16: 20 us), read and written, where a copy reaches 4.7 to 5.4 by its size.
 #include "block_rows.h"
 
 namespace qvggt {

@@ -2,7 +2,7 @@
 //     x' = x + scale gate[r] norm_post(y),      h = norm_pre(x') (1 + mod_scale[r]) + mod_shift[r].
 //
 // One pass: LANES lanes have a row, every one V pieces of eight channels, in registers from the first load to the last store; means and variances are two passes over registers.  Bound by memory:
-// 5.4 to 5.9 TB/s, read and written, from 128 to 8192 channels (137400 rows of 1024 in bf16: 192 us), where a copy reaches 4.8 to 5.0; 4.5 with gains, gate, scale and shift of everything, which are
+// 5.4 to 5.9 TB/s, read and written, from 128 to 8192 channels (137400 rows of 1024 in bf16: 192 us), where a copy reaches 4.7 to 5.4 by its size; 4.8 with gains, gate, scale and shift of everything, which are
 // more bytes a row than the row itself, out of L2.
 #include "block_rows.h"
 
