@@ -547,7 +547,8 @@ int qvggt_kv4_attention(const void *Q, int q_dtype, int T, long long q_stride, i
  *
  * qvggt_attention:  for every sequence b, its n = q_starts[b + 1] - q_starts[b] query tokens (rows q_starts[b] .. of Q) over its len keys and values, rows kv_starts[b] .. of K and V:
  *     out[i, h, :] = sum_j softmax_j( scale * <q[i, h], k[j, h']> ) v[j, h'],     h' = h / (q_heads / kv_heads),
- *   j over the keys 0 .. len - n + i with causal = 1 (the queries are the sequence's last n tokens), 0 .. len - 1 with causal = 0.  A query that sees no key gives zeros.
+ *   j over the keys 0 .. len - n + i with causal = 1 (the queries are the sequence's last n tokens), 0 .. len - 1 with causal = 0.  A query that sees no key gives zeros,
+ *   one that sees keys and is no number (an infinity or a NaN in its head), or whose scores are all -infinity, NaN.
  *   |scale| <= 1e38.  dtype: QVGGT_BF16, of Q, K, V and out.  Q [T, q_heads, d], K and V [S, kv_heads, d] at their strides (elements, multiples of 8; k_stride and v_stride below 2^24);
  *   d = 64 or 128; q_heads a
  *   multiple of kv_heads.  q_starts: int32 [seqs + 1], not falling.  kv_lens = NULL: kv_starts is int32 [seqs + 1] and len the difference (whole prompts: kv_starts = q_starts); otherwise

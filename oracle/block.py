@@ -115,7 +115,9 @@ def attention(q, k, v, scale, causal, lengths, starts, max_q=None, max_kv=None):
                 if causal:
                     hidden = torch.arange(looked, device=q.device) > m - n + lo + torch.arange(len(some), device=q.device)[:, None]
                     x, terms = x.masked_fill(hidden, -math.inf), terms.masked_fill(hidden, 0.0)
-                p = torch.nan_to_num(torch.softmax(x, -1))
+                # a row that sees no key is zeros, one whose scores are all -infinity no number
+                sees = torch.ones_like(x, dtype=torch.bool) if not causal else ~hidden
+                p = torch.where(sees.any(-1, keepdim=True), torch.softmax(x, -1), 0.0)
                 o = p @ vv
                 e = (d + 8) * U * terms.amax(-1, keepdim=True) * 2 + 8 * U
                 # sum p |v - o|, a channel at a time where that is much

@@ -64,6 +64,8 @@ __device__ inline Sequence sequence_of(const Attention &a, int b)
 }
 // Keys that query i sees.
 __device__ inline int visible(const Attention &a, const Sequence &s, int i) { return a.causal ? min(max(s.len - s.total + i + 1, 0), s.limit) : s.limit; }
+// What a row's sums are multiplied by.  A row without keys is zeros; the weights of one that sees keys add up to 0 where all its scores are -infinity, which have no softmax.
+__device__ inline float share_of(float total, int seen) { return total != 0.0f ? 1.0f / total : seen > 0 ? __builtin_nanf("") : 0.0f; }
 
 // ---- how rows lie in LDS
 template <int D, int M>
@@ -491,7 +493,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attention_own_rows_kerne
     }
     const float total = r.total(0);
     if (w.splits == 1) {
-        const float f = total != 0.0f ? 1.0f / total : 0.0f;        // (a row that is no number has a total that is none)
+        const float f = share_of(total, r.end[0]);
         const int i = row / w.group;
         uint16_t *const to = a.out + ((long long)(seq.q0 + i) * a.q_heads + head * w.group + row - i * w.group) * D;
         // Of sixteen channels, of which the two lanes of a row have fours in turn, each comes to have eight neighbouring ones
@@ -614,8 +616,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 2 : 1) void attention_few_
             x = make_float4(fmaf(f, y.x, x.x), fmaf(f, y.y, x.y), fmaf(f, y.z, x.z), fmaf(f, y.w, x.w));
         }
         if (w.splits == 1) {
-            const float f = all != 0.0f ? 1.0f / all : 0.0f;
             const int at = row / w.group;
+            const float f = share_of(all, visible(a, seq, at));
             *reinterpret_cast<uint2 *>(a.out + ((long long)(seq.q0 + at) * a.q_heads + head * w.group + row - at * w.group) * D + 4 * c) =
                 make_uint2(pack_bf16x2(x.x * f, x.y * f), pack_bf16x2(x.z * f, x.w * f));
         } else {
@@ -638,7 +640,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(Cut w)
     const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, b = rest / blocks, row = rest % blocks * 16 + (threadIdx.x >> 4);
     const Sequence seq = sequence_of(a, b);
     if (row >= seq.n * w.group) return;
-    const int i = row / w.group, used = (visible(a, seq, i) + w.chunk - 1) / w.chunk;
+    const int i = row / w.group, seen = visible(a, seq, i), used = (seen + w.chunk - 1) / w.chunk;
     const float *const from = w.partials + partial_row(w, b, head, row, 0) * kPartial<D>;
     float *const mine = factors[threadIdx.x >> 4];
     float top = kNone, total = 0.0f, x[C];
@@ -667,7 +669,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(Cut w)
             x[c + 1] = fmaf(f, v.y, x[c + 1]);
         }
     }
-    const float f = total != 0.0f ? 1.0f / total : 0.0f;
+    const float f = share_of(total, seen);
     uint32_t *const to = reinterpret_cast<uint32_t *>(a.out + ((long long)(seq.q0 + i) * a.q_heads + head * w.group + row - i * w.group) * D + first);
 #pragma unroll
     for (int c = 0; c < C; c += 2) to[c / 2] = pack_bf16x2(x[c] * f, x[c + 1] * f);

@@ -74,3 +74,14 @@ def test_residual_is_its_formula():
         n = (want - mean) / math.sqrt(float(((want - mean) ** 2).mean()) + 1e-5) * v[3].double() + v[4].double()
         assert torch.allclose(s[t], want, atol=1e-12) and torch.allclose(h[t], n * (1 + v[4 + r].double()) + v[1 + r].double(), atol=1e-12)
     assert float(s_off.max()) < 1e-4 and float(h_off.max()) < 1e-3
+
+
+def test_attention_of_infinite_scores():
+    """Zeros are for rows without keys only."""
+    q, k, v = (torch.randn(4, 1, 4, generator=torch.Generator().manual_seed(i)) for i in range(3))
+    k[:, :, 1] = k[:, :, 1].abs() + 1
+    q[2, 0, 1] = -math.inf
+    got, _ = O.attention(q, k, v, 1.0, True, [(4, 3)], [0])
+    assert bool((got[0] == 0).all()) and bool(torch.isnan(got[2]).all()) and bool(torch.isfinite(got[[1, 3]]).all())
+    got, _ = O.attention(q, k, v, 1.0, False, [(4, 3)], [0])
+    assert bool(torch.isnan(got[2]).all()) and bool(torch.isfinite(got[[0, 1, 3]]).all())
