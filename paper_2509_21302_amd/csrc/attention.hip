@@ -12,7 +12,10 @@
 // The running maximum of a row is raised when scores exceed it by much: weights are at most 2^8 or 2^12 then, which costs bf16 and fp32 nothing, and sums are multiplied by a factor in few steps.
 // In the steps that all rows of a block see it is not even looked for: the sum of a step's weights says whether one of them is too large, and only then are they made again (what that saves is 12 %
 // of the vector instructions: 13740 rows on as many keys, 16 heads x 64, 809 us for 856; 8192 on 8192, 16 x 128, 485 for 501).  Weights are rounded to bf16 (to nearest), for the product and for the sum
-// that it is divided by alike.  A row starts from a maximum of -3e38 over the scale (over 1 for small ones), so that rows that see nothing end with a sum of 0.
+// that it is divided by alike.  A row starts from a maximum of the lowest number, so that rows that see nothing end with a sum of 0.
+//
+// A weight's exponent is one multiplication and addition, score * scale2 - maximum * scale2, as long as the second product is small: at 2^12 its rounding is 2^-13 of an exponent, at 2^31 whole weights, and past
+// fp32 all of them.  Rows of larger ones have differences of scores instead, times the scale, which are right at any scale (one instruction more a score, and only where there are such rows).
 #include <type_traits>
 
 #include "attention.h"
@@ -34,15 +37,14 @@ union Operand {
     bf16x8 b;
 };
 
-constexpr float kNone = -3.0e38f, kLog2e = 1.4426950408889634f;
-constexpr float kSlack = 8.0f, kMostWeights = 4096.0f;       // log2 of a weight; a lane's weights of a step
+constexpr float kNone = -3.4028235e38f, kLog2e = 1.4426950408889634f;       // kNone: the maximum that a row starts from
+constexpr float kSlack = 8.0f, kMostWeights = 4096.0f;       // log2 of a weight; a lane's weights of a step, and the maximum * scale2 from which they are of differences
 
 struct Cut {
     Attention a;
     int group, chunk, splits, tiles;        // query heads of a key head; keys of a part; parts and tiles of rows that there may be
     float scale2;                           // |scale| log2(e); its sign, and a scale of 0, are in the queries
     uint32_t flip, keep;                    // ... as masks of pairs of them
-    float none;                             // the maximum that a row starts from: times scale2 it is a number, so that an unseen key's weight is 0 by it
     float *partials;                        // [seqs][key heads][rows][splits][D + 2]: a row's sums, maximum and weights' sum
 };
 
@@ -102,7 +104,7 @@ struct Wave {
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
             const int row = row0 + M * n + lane % M, r = min(row, rows - 1), i = r / w.group;
-            top[n] = w.none;
+            top[n] = kNone;
             sum[n] = 0.0f;
             end[n] = row < rows ? visible(w.a, s, i) : 0;
             const uint16_t *const from = w.a.q + (long long)(s.q0 + i) * w.a.q_stride + (head * w.group + r - i * w.group) * D + 8 * g;
@@ -195,20 +197,20 @@ struct Wave {
         for (int n = 0; n < NQ; ++n) any |= higher[n] = (m[n] - top[n]) * scale2 > kSlack;
         if (__builtin_amdgcn_ballot_w64(any)) raise(m, higher, scale2);
     }
-    // Where a row's weights of a step, of which each of its lanes has a sum, are too large (or no numbers); whether there is such a row.
+    // Where a row's weights of a step, of which each of its lanes has a sum, are too large, or its maximum is far out; whether there is such a row.
     template <int NK>
     __device__ bool raise_by(const float (&s)[NQ], const Sums (&x)[NK][NQ], float scale2)
     {
-        bool any = false;
+        bool any = false, higher_here[NQ];
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) any |= !(s[n] <= kMostWeights);
+        for (int n = 0; n < NQ; ++n) any |= higher_here[n] = !(fmaxf(s[n], fabsf(top[n] * scale2)) <= kMostWeights);       // (a sum that is no number stays one without this)
         if (!__builtin_amdgcn_ballot_w64(any)) return false;
         float m[NQ];
         bool higher[NQ];
         largest(x, m);
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
-            uint32_t mine = !(s[n] <= kMostWeights);
+            uint32_t mine = higher_here[n];
             if (M == 16) {
                 const auto r = __builtin_amdgcn_permlane16_swap(mine, mine, false, false);
                 mine = r[0] | r[1];
@@ -219,21 +221,51 @@ struct Wave {
         raise(m, higher, scale2);
         return true;
     }
-    // Weights of NK tiles of keys, as operands, and the lane's sums of them.
+    // Weights of NK tiles of keys, as operands, and the lane's sums of them: without rows that are far out, and with any.
     template <int NK>
-    __device__ void weights(const Sums (&x)[NK][NQ], float scale2, Operand (&p)[NK * M / kKeys][NQ], float (&s)[NQ])
+    __device__ void weights(const Sums (&x)[NK][NQ], float scale2, Operand (&p)[NK * M / kKeys][NQ], float (&s)[NQ]) const
+    {
+        float off[NQ];
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) off[n] = top[n] * scale2;
+        weights(x, scale2, off, p, s);
+    }
+    template <int NK>
+    __device__ void weights_of_any(Sums (&x)[NK][NQ], float scale2, Operand (&p)[NK * M / kKeys][NQ], float (&s)[NQ]) const
+    {
+        // (a row that has seen nothing has weights of 0 from any finite `off`)
+        float off[NQ];
+        bool far[NQ], any = false;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            off[n] = fmaxf(top[n] * scale2, kNone);
+            any |= far[n] = fabsf(off[n]) > kMostWeights && top[n] > kNone;
+        }
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(any) != 0, 0))
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                const float from = far[n] ? top[n] : 0.0f;
+                off[n] = far[n] ? 0.0f : off[n];
+#pragma unroll
+                for (int k = 0; k < NK; ++k)
+#pragma unroll
+                    for (int i = 0; i < kSums; ++i) x[k][n][i] -= from;
+            }
+        weights(x, scale2, off, p, s);
+    }
+    template <int NK>
+    __device__ static void weights(const Sums (&x)[NK][NQ], float scale2, const float (&off)[NQ], Operand (&p)[NK * M / kKeys][NQ], float (&s)[NQ])
     {
         bf16x2 one;
         one[0] = one[1] = (__bf16)1.0f;
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
-            const float off = top[n] * scale2;
             s[n] = 0.0f;
 #pragma unroll
             for (int k = 0; k < NK; ++k)
 #pragma unroll
                 for (int i = 0; i < kSums; i += 2) {
-                    const float a = __builtin_amdgcn_exp2f(fmaf(x[k][n][i], scale2, -off)), b = __builtin_amdgcn_exp2f(fmaf(x[k][n][i + 1], scale2, -off));
+                    const float a = __builtin_amdgcn_exp2f(fmaf(x[k][n][i], scale2, -off[n])), b = __builtin_amdgcn_exp2f(fmaf(x[k][n][i + 1], scale2, -off[n]));
                     const uint32_t both = pack_bf16x2(a, b);
                     p[(k * kSums + i) / 8][n].w[(k * kSums + i) % 8 / 2] = both;
                     s[n] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, both), one, s[n], false);
@@ -446,7 +478,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attention_own_rows_kerne
             r.scores(keys + kNext * kTile, y);
             r.weights(x, w.scale2, p, s);
             pace_scores<D>();
-            if (r.raise_by(s, x, w.scale2)) r.weights(x, w.scale2, p, s);
+            if (r.raise_by(s, x, w.scale2)) r.weights_of_any(x, w.scale2, p, s);
             r.sum[0] += s[0];
 #pragma unroll
             for (int i = 0; i < 4; ++i) r.add(values + kHere * kTile + 16 * i * R::kBytes, p[i]);
@@ -474,7 +506,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attention_own_rows_kerne
                 bad = __syncthreads_or(find_no_numbers(mine, kTile, threadIdx.x, 256));
             }
             r.raise_to(x, w.scale2);
-            r.weights(x, w.scale2, p, s);
+            r.weights_of_any(x, w.scale2, p, s);
             r.sum[0] += s[0];
             if (bad) {
                 r.add_no_numbers(mine, t, kKeys);
@@ -517,7 +549,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attention_own_rows_kerne
         for (int c = 0; c < D / 32; ++c)
 #pragma unroll
             for (int e = 0; e < 16; e += 2) *reinterpret_cast<float2 *>(to + 32 * c + 8 * (e / 4) + 4 * r.g + e % 4) = make_float2(r.o[c][0][e], r.o[c][0][e + 1]);
-        if (r.g == 0) *reinterpret_cast<float2 *>(to + D) = make_float2(r.top[0] * w.scale2, total);
+        if (r.g == 0) *reinterpret_cast<float2 *>(to + D) = make_float2(r.top[0], total);
     }
 }
 
@@ -570,7 +602,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 2 : 1) void attention_few_
         const bool masked = t + kKeys > full;
         if (masked) r.hide(x, t);
         r.raise_to(x, w.scale2);
-        r.weights(x, w.scale2, p, s);
+        r.weights_of_any(x, w.scale2, p, s);
 #pragma unroll
         for (int n = 0; n < NQ; ++n) r.sum[n] += s[n];
         if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kEach) : "memory");
@@ -604,7 +636,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 2 : 1) void attention_few_
     __syncthreads();
     for (int i = threadIdx.x; i < rows * kFours; i += 64 * WAVES) {
         const int row = i / kFours, c = i % kFours;
-        float top = w.none, all = 0.0f;
+        float top = kNone, all = 0.0f;
 #pragma unroll
         for (int n = 0; n < WAVES; ++n) top = fmaxf(top, tops[n][row]);
         float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -624,7 +656,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 2 : 1) void attention_few_
             float *const to = w.partials + partial_row(w, b, head, row, split) * kPartial<D>;
             *reinterpret_cast<float2 *>(to + 4 * c) = make_float2(x.x, x.y);
             *reinterpret_cast<float2 *>(to + 4 * c + 2) = make_float2(x.z, x.w);
-            if (c == 0) *reinterpret_cast<float2 *>(to + D) = make_float2(top * w.scale2, all);
+            if (c == 0) *reinterpret_cast<float2 *>(to + D) = make_float2(top, all);
         }
     }
 }
@@ -648,7 +680,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(Cut w)
     top = max_over_16_lanes(top);
     for (int s = lane; s < used; s += 16) {
         const float2 p = *reinterpret_cast<const float2 *>(from + (size_t)s * kPartial<D> + D);
-        mine[s] = __builtin_amdgcn_exp2f(p.x - top);
+        mine[s] = __builtin_amdgcn_exp2f((p.x - top) * w.scale2);
         total = fmaf(mine[s], p.y, total);
     }
     lanes_exchange_fence();
@@ -686,7 +718,7 @@ hipError_t launch(const Attention &a, hipStream_t stream)
     const int group = a.q_heads / a.kv_heads;
     const AttentionPlan p = attention_plan(a.seqs, a.max_q, a.max_kv, a.q_heads, a.kv_heads, D, a.causal);
     const float scale2 = a.scale == 0.0f ? 1.0f : __builtin_fabsf(a.scale) * kLog2e;
-    const Cut w{a, group, p.chunk, p.splits, p.tiles, scale2, a.scale < 0.0f ? 0x80008000u : 0u, a.scale == 0.0f ? 0u : 0xffffffffu, scale2 > 1.0f ? kNone / scale2 : kNone,
+    const Cut w{a, group, p.chunk, p.splits, p.tiles, scale2, a.scale < 0.0f ? 0x80008000u : 0u, a.scale == 0.0f ? 0u : 0xffffffffu,
                 static_cast<float *>(a.workspace)};
     const dim3 grid((unsigned)a.seqs * a.kv_heads * p.tiles * p.splits);
     hipError_t e = p.few ? prepare_device() : hipSuccess;
