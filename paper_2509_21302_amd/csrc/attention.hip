@@ -43,8 +43,9 @@ constexpr float kSlack = 8.0f, kMostWeights = 4096.0f;       // log2 of a weight
 struct Cut {
     Attention a;
     int group, chunk, splits, tiles;        // query heads of a key head; keys of a part; parts and tiles of rows that there may be
-    float scale2;                           // |scale| log2(e); its sign, and a scale of 0, are in the queries
-    uint32_t flip, keep;                    // ... as masks of pairs of them
+    float scale2;                           // |scale| log2(e), 1 for a scale of 0; its sign, and a scale of 0, are in the queries
+    uint32_t flip;                          // ... the sign as a mask of pairs of them
+    int zero;                               // ... whether the scale is 0: queries of 0, or NaN where they are no numbers
     float *partials;                        // [seqs][key heads][rows][splits][D + 2]: a row's sums, maximum and weights' sum
 };
 
@@ -81,6 +82,9 @@ struct Rows {
         return D == 128 ? c ^ (row & 3) << 2 : c ^ (row >> 1 & 1) << 2;
     }
 };
+
+// A pair of bf16 times 0.
+__device__ inline uint32_t none_of(uint32_t w) { return ((w & 0x7f80u) == 0x7f80u ? 0x7fc0u : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0x7fc00000u : 0u); }
 
 __device__ inline float4v product(const Operand &a, const Operand &b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.b, b.b, c, 0, 0, 0); }
 __device__ inline float16v product(const Operand &a, const Operand &b, float16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.b, b.b, c, 0, 0, 0); }
@@ -119,7 +123,14 @@ struct Wave {
 #pragma unroll
             for (int k = 0; k < kSteps; ++k)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) q[n][k].w[j] = (q[n][k].w[j] & w.keep) ^ w.flip;
+                for (int j = 0; j < 4; ++j) q[n][k].w[j] ^= w.flip;
+        if (__builtin_expect(w.zero, 0))
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) q[n][k].w[j] = none_of(q[n][k].w[j]);
 #pragma unroll
         for (int c = 0; c < kTiles; ++c)
 #pragma unroll
@@ -718,7 +729,7 @@ hipError_t launch(const Attention &a, hipStream_t stream)
     const int group = a.q_heads / a.kv_heads;
     const AttentionPlan p = attention_plan(a.seqs, a.max_q, a.max_kv, a.q_heads, a.kv_heads, D, a.causal);
     const float scale2 = a.scale == 0.0f ? 1.0f : __builtin_fabsf(a.scale) * kLog2e;
-    const Cut w{a, group, p.chunk, p.splits, p.tiles, scale2, a.scale < 0.0f ? 0x80008000u : 0u, a.scale == 0.0f ? 0u : 0xffffffffu,
+    const Cut w{a, group, p.chunk, p.splits, p.tiles, scale2, a.scale < 0.0f ? 0x80008000u : 0u, a.scale == 0.0f,
                 static_cast<float *>(a.workspace)};
     const dim3 grid((unsigned)a.seqs * a.kv_heads * p.tiles * p.splits);
     hipError_t e = p.few ? prepare_device() : hipSuccess;

@@ -132,3 +132,21 @@ def test_far_scales_of_small_queries_and_keys(d, n, m, group):
     K[:] = K * 2.0 ** -60
     Q[:] = Q * 2.0 ** -30
     assert torch.equal(attend(Q, K, V, 0.125 * 2.0 ** 90, True, whole([0, n]), whole([0, m]), None, n, m), want)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n,m,group", KERNELS)
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("scale", [0.0, -0.0])
+def test_a_scale_of_zero_makes_no_number_of_an_infinite_query(d, n, m, group, bad, scale):
+    """0 times a score that is no number is none; rows of numbers are the mean of the values they see."""
+    Q, K, V = inputs(n, m, 2 * group, 2, d, n + m)
+    Q[n // 2, group, 7] = bad
+    Q[n - 1, 0, d - 2] = bad
+    got = attend(Q, K, V, scale, True, whole([0, n]), whole([0, m]), None, n, m)
+    rows = torch.zeros(n, 2 * group, dtype=torch.bool, device=DEV)
+    rows[n // 2, group] = rows[n - 1, 0] = True
+    assert bool(torch.isnan(got[rows].float()).all())
+    Q[n // 2, group, 7] = Q[n - 1, 0, d - 2] = 0.0
+    want, off = O.attention(Q, K, V, 0.0, True, [(n, m)], [0])
+    near(got[~rows], want[~rows], off[~rows])
