@@ -919,7 +919,7 @@ int qvggt_kv4_attention(const void *Q, int q_dtype, int T, long long q_stride, i
     if (!valid_pages(num_pages, page_tokens, kv_heads, d) || !valid_attention(T, seqs, max_q, max_kv, q_heads, kv_heads, d) || q_stride < 0 ||
         !valid_rope(rope, rope_rows, rope_dim, rope_pair, d) || table_width < 0 || max_kv > (long long)table_width * page_tokens || (max_kv > 0 && num_pages == 0))
         return QVGGT_ERR_SHAPE;
-    if (!(std::fabs(scale) <= 1e38f) || (causal != 0 && causal != 1)) return QVGGT_ERR_ARG;
+    if (!std::isfinite(scale) || (causal != 0 && causal != 1)) return QVGGT_ERR_ARG;
     if (T == 0 || seqs == 0 || max_q == 0) return QVGGT_OK;
     const size_t need = qvggt::kv4_attention_workspace_bytes(seqs, max_q, max_kv, q_heads, kv_heads, d);
     if (!Q || !q_starts || !kv_lens || !out || (rope && !positions) || (max_kv > 0 && (!cache || !page_table)) || (need > 0 && !workspace)) return QVGGT_ERR_NULL;

@@ -66,3 +66,9 @@ def test_binding_refuses_host_tensors():
         q.qvggt_kv4_append(x, x, None, one, torch.zeros(1, 16 * 68, dtype=torch.uint8), 16)
     with pytest.raises(ValueError):
         q.qvggt_kv4_attention(x, None, 1.0, True, torch.zeros(1, 16 * 68, dtype=torch.uint8), 16, 1, torch.zeros(1, 1, dtype=torch.int32), one, one[:1], 2, 2, x, None)
+
+
+@pytest.mark.parametrize("scale", [1.1e38, -3.4e38])
+def test_attention_takes_every_finite_scale(scale):
+    """(Of a call without tokens, which returns behind the check.)"""
+    assert call("attention", scale=scale, T=0) == OK and call("attention", scale=float("inf"), T=0) == ARG
