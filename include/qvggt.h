@@ -555,7 +555,7 @@ int qvggt_kv4_attention(const void *Q, int q_dtype, int T, long long q_stride, i
  *   kv_starts and kv_lens are int32 [seqs] (a buffer for every sequence that its tokens are added to, for example).  Starts and lengths are read on the device: a call can be captured and replayed
  *   with others.  Those that lead outside of T and S are cut.  max_q and max_kv: at least every n and len (they decide how the work is cut up; of a longer sequence the first max_q queries are
  *   answered, each from those of the first max_kv keys that it would see).  Rows of K and V that no sequence names, or that no query sees, may be anything.  seqs <= 65535.
- *   out: bf16 [T, q_heads, d]; rows of no sequence are not written.  It overlaps no input.  workspace: qvggt_attention_workspace_bytes of the same sizes, 16-byte aligned, NULL where that is 0;
+ *   out: bf16 [T, q_heads, d]; rows of no sequence are not written.  It overlaps no input (QVGGT_ERR_ARG where it begins at the address of Q, K or V).  workspace: qvggt_attention_workspace_bytes of the same sizes, 16-byte aligned, NULL where that is 0;
  *   two calls that may run at the same time take one each.  Scores, maxima and sums are fp32; a weight is of a score's difference from the maximum, so scores times the scale may pass fp32.  Weights are rounded to the nearest bf16 (8 bits), in the sum that they are divided by as well.  Sums in
  *   a fixed order: the same call gives the same bits.  max_kv at most 2^30, seqs * kv_heads * ceil(max_q * (q_heads / kv_heads) / 32) at most 2^23.  int32 arrays need 4-byte alignment only.
  *

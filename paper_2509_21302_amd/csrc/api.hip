@@ -993,6 +993,8 @@ int qvggt_attention(const void *Q, const void *K, const void *V, int dtype, int 
         !aligned4(kv_lens) || !aligned16(out) || !aligned16(workspace))
         return QVGGT_ERR_ALIGN;
     if (workspace_bytes < need) return QVGGT_ERR_WORKSPACE;
+    // blocks write results while others still read
+    if (out == Q || (max_kv > 0 && (out == K || out == V))) return QVGGT_ERR_ARG;
     const qvggt::Attention a{static_cast<const uint16_t *>(Q), static_cast<const uint16_t *>(K), static_cast<const uint16_t *>(V), q_stride, k_stride, v_stride, T, S, q_heads, kv_heads, scale,
                              causal, q_starts, kv_starts, kv_lens, seqs, max_q, max_kv, static_cast<uint16_t *>(out), workspace};
     return hip_status(qvggt::run_attention(a, d, static_cast<hipStream_t>(stream)));

@@ -69,6 +69,11 @@ def test_scales_that_leave_fp32(scale):
     assert call("attention", scale=scale) == ARG
 
 
+@pytest.mark.parametrize("other", [dict(out=P), dict(out=2 * P), dict(out=3 * P), dict(out=3 * P, heads=8, ws=None, size=0), dict(out=P, T=1, S=0, max_kv=0)])
+def test_attention_output_in_the_place_of_an_input(other):
+    assert call("attention", **dict(dict(Q=P, K=2 * P, V=3 * P, out=4 * P), **other)) == ARG
+
+
 def test_workspace():
     size = q.qvggt_attention_workspace_bytes
     need = size(1, 1, 1, 131072, 32, 8, 128)
