@@ -121,7 +121,10 @@ def attention(q, k, v, scale, causal, lengths, starts, max_q=None, max_kv=None):
                 o = p @ vv
                 e = (d + 8) * U * terms.amax(-1, keepdim=True) * 2 + 8 * U
                 # sum p |v - o|, a channel at a time where that is much
-                spread = torch.stack([(p * (vv[:, c] - o[:, c:c + 1]).abs()).sum(1) for c in range(d)], 1)
+                if p.numel() * d <= 1 << 24:
+                    spread = (p[:, :, None] * (vv[None] - o[:, None]).abs()).sum(1)
+                else:
+                    spread = torch.stack([(p * (vv[:, c] - o[:, c:c + 1]).abs()).sum(1) for c in range(d)], 1)
                 sums = (looked + 64) * U * (p @ vv.abs() + o.abs())
                 at = slice(row + lo, row + lo + len(some))
                 out[at, h] = o
