@@ -513,8 +513,8 @@ int qvggt_calib_descent_step(float *theta, const float *grad, int n, float lr, f
  *   queries are answered, each from those of the first max_kv keys that it would see), max_kv <= table_width * page_tokens.  What lies in pages behind a sequence's end, and entries of page_table behind its last page, may be anything.  An entry in use that is no page of
  *   the pool gives wrong results for its sequence, and nothing is read outside the pool.  seqs <= 65535.  out: bf16 [T, q_heads, d]; rows of no sequence are not written.
  *   workspace: qvggt_kv4_attention_workspace_bytes of the same sizes, 16-byte aligned, NULL where that is 0.  Scores, weights and sums are fp32, queries (float32 ones too) and weights
- *   times the values' steps are rounded to the nearest fp16 (11 bits) for the products; those weights reach down to 2^-31 of the largest at the largest step that the row sees.  Sums in a
- *   fixed order: the same call gives the same bits.
+ *   times the values' steps are rounded to the nearest fp16 (11 bits) for the products (numbers of a turned
+ *   query times scale * log2(e) over 2^19 are taken as that); those weights reach down to 2^-31 of the largest at the largest step that the row sees.  Sums in a fixed order: the same call gives the same bits.
  * T * heads at most 2^27 in qvggt_kv4_append and qvggt_kv4_read; in qvggt_kv4_attention max_kv at most 2^30 and seqs * kv_heads * ceil(max_q * (q_heads / kv_heads) / 64) at most 2^23.
  * QVGGT_ERR_SHAPE for sizes outside these limits, QVGGT_ERR_ARG for a scale that is not finite or a causal other than 0 and 1.  int32 arrays and tables need 16-byte aligned pointers as
  * everything else.
@@ -535,7 +535,8 @@ int qvggt_kv4_attention(const void *Q, int q_dtype, int T, long long q_stride, i
  * What stands between and around the layers of a block that keeps no cache: heads of queries and keys normalised and rotated, attention of whole sequences, the residual stream with its norms.
  * A norm (QVGGT_NORM_*) of n channels is (x - mean) / sqrt(variance + eps), x / sqrt(mean of squares + eps), or x as it is; then times a gain and plus a bias (f32 [n], NULL: without;
  * with QVGGT_NORM_NONE too).  eps >= 0.  Arithmetic, sums and statistics are fp32, results are rounded once, to the nearest.  An infinity or a NaN stays in its own row (head), and in the rows
- * of attention that see it.
+ * of attention that see it.  Sums are not guarded against leaving fp32: a row that a norm is taken of needs squares whose sum is in its range (values up to 1e17; with eps = 0, from 1e-18 on), and the
+ * values of attention, times 2^12 and the number of keys, need to be.
  *
  * qvggt_heads_norm_rope:  every head of T tokens' queries and keys (d = 64 or 128 channels): norm, then the rotation of qvggt_kv4_append by positions with several axes: the angle number p
  *   of a token is the one at column p of row positions[axis][token] of the table, axis = pair_axis[p], or p * axes / (rope_dim / 2) where pair_axis is NULL (sections of equal length, one
@@ -555,9 +556,10 @@ int qvggt_kv4_attention(const void *Q, int q_dtype, int T, long long q_stride, i
  *   kv_starts and kv_lens are int32 [seqs] (a buffer for every sequence that its tokens are added to, for example).  Starts and lengths are read on the device: a call can be captured and replayed
  *   with others.  Those that lead outside of T and S are cut.  max_q and max_kv: at least every n and len (they decide how the work is cut up; of a longer sequence the first max_q queries are
  *   answered, each from those of the first max_kv keys that it would see).  Rows of K and V that no sequence names, or that no query sees, may be anything.  seqs <= 65535.
- *   out: bf16 [T, q_heads, d]; rows of no sequence are not written.  It overlaps no input (QVGGT_ERR_ARG where it begins at the address of Q, K or V).  workspace: qvggt_attention_workspace_bytes of the same sizes, 16-byte aligned, NULL where that is 0;
- *   two calls that may run at the same time take one each.  Scores, maxima and sums are fp32; a weight is of a score's difference from the maximum, so scores times the scale may pass fp32.  Weights are rounded to the nearest bf16 (8 bits), in the sum that they are divided by as well.  Sums in
- *   a fixed order: the same call gives the same bits.  max_kv at most 2^30, seqs * kv_heads * ceil(max_q * (q_heads / kv_heads) / 32) at most 2^23.  int32 arrays need 4-byte alignment only.
+ *   out: bf16 [T, q_heads, d]; rows of no sequence are not written.  It overlaps no input (QVGGT_ERR_ARG where it begins at the address of Q, K or V).  workspace: qvggt_attention_workspace_bytes of the
+ *   same sizes, 16-byte aligned, NULL where that is 0; two calls that may run at the same time take one each.  Scores, maxima and sums are fp32; a weight is of a score's difference from the maximum, so scores times
+ *   the scale may pass fp32.  Weights are rounded to the nearest bf16 (8 bits), in the sum that they are divided by as well.  Sums in a fixed order: the same call gives the
+ *   same bits.  max_kv at most 2^30, seqs * kv_heads * ceil(max_q * (q_heads / kv_heads) / 32) at most 2^23.  int32 arrays need 4-byte alignment only.
  *
  * qvggt_residual_norm:  of M tokens of C channels (a multiple of 8 from 8 to 8192), y a block's output, x the residual stream:
  *     x'[t] = x[t] + scale * gate[r] * norm_post(y[t]),       h[t] = norm(x'[t]) * (1 + mod_scale[r]) + mod_shift[r]

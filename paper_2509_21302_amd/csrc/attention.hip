@@ -299,7 +299,7 @@ struct Wave {
         }
     }
     // A value that is no number touches only the rows that see it: where `keys` rows of values have one and some rows of the wave do not see all of those keys, it is added to the rows that
-    // do, here, before it is taken out of LDS.  A weight is never 0, so an infinity stays one.
+    // do, here, before it is taken out of LDS: a weight is above 0, though exp2 of a far score is not, so an infinity stays one.  (In steps that all rows see the product has it: of a weight of 0, NaN.)
     __device__ void add_no_numbers(const char *values, int t, int keys)
     {
         for (int key = 0; key < keys; ++key)
@@ -406,8 +406,8 @@ __device__ inline void pace_values()
 
 // ---- many rows: a wave has 32 of its own, the four waves of a block go through the same keys, 64 a step, two tiles of each in LDS.  Products of 32 x 32 x 16: a lane's registers hold a tile and
 // the scores of the next one, for which 16 x 16 x 32, faster out of registers alone, leave no room (8192 rows on 8192 keys, 16 heads x 128: 516 us for 493).  Bound by the board's power where sequences are
-// long: 11003 tokens, 32 heads on 8 x 128, 837 to 887 us by the board, 1.12 to 1.19 PFLOP/s at 1.6 GHz, with the matrix cores busy in 0.65 of the cycles, and 651 us on zeros; with 64 channels by vector
-// instructions as well (96 for 16 products a step: 13740 rows on as many keys, 16 heads, 765 to 805 us, 0.96 to 1.01 PFLOP/s).  A block costs some 8 us besides its steps.
+// long: 11003 tokens, 32 heads on 8 x 128, 877 to 902 us by the board, 1.10 to 1.13 PFLOP/s at 1.6 GHz, with the matrix cores busy in 0.65 of the cycles, and 651 us on zeros; with 64 channels by vector
+// instructions as well (97 for 16 products a step: 13740 rows on as many keys, 16 heads, 798 to 816 us, 0.95 to 0.97 PFLOP/s).  A block costs some 8 us besides its steps.
 template <int D>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attention_own_rows_kernel(Cut w)
 {
@@ -565,7 +565,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attention_own_rows_kerne
 }
 
 // ---- few rows (32 at most): the waves of a block share them and go through keys of their own, 32 at a time, brought into LDS by each for itself.  Products of 16 x 16 x 32, of whose rows fewer are
-// nobody's.  Bound by memory: 48 rows on up to 8192 keys, 32 heads on 8 x 128, 147 us, 5.8 TB/s; a block alone on a CU brings in 52 GB/s (one row on 601 keys: 7.3 us)
+// nobody's.  Bound by memory: 48 rows on up to 8192 keys, 32 heads on 8 x 128, 148 us, 5.8 TB/s; a block alone on a CU brings in 52 GB/s (one row on 601 keys: 7.4 us)
 template <int D, int NQ, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 2 : 1) void attention_few_rows_kernel(Cut w)
 {

@@ -5,7 +5,9 @@
 namespace qvggt {
 
 constexpr int kAttentionTile = 32;                  // rows of a wave, query tokens times the query heads that share a key head, where a block has four times as many
-constexpr int kAttentionFewRows = 32;               // rows of a key head up to which a block's waves share them
+// Rows of a key head up to which a block's waves share them, which is what their registers hold.  32 rows that way and as many rows: 16384 keys of one sequence, 8 key heads x 128, 21.6 us and 26.5 (64 channels
+// 13.7 and 20.4; 36 rows 27.7 and 21.2); 256 sequences of 256 keys 57.5 and 64.4.  The other way round where many sequences of many keys leave none to be cut: 64 of 2048 keys 125 and 102 (16 rows 111 and 102, 8 rows 101 and 103)
+constexpr int kAttentionFewRows = 32;
 constexpr long long kAttentionMostBlocks = 1 << 23; // of a launch
 constexpr int kAttentionKeys = 128;                 // parts of the keys are multiples of it
 constexpr int kAttentionMostParts = 256;            // of a sequence's keys
@@ -60,7 +62,7 @@ inline AttentionPlan attention_plan(int seqs, int max_q, int max_kv, int q_heads
         n = n == 1 ? 2 : i % 2 ? n / 2 * 3 : n / 3 * 4;
     }
     p.splits = max_kv > 0 ? (int)attention_div_up(max_kv, p.chunk) : 1;
-    // Whole sequences of few rows, a CU for each: eight waves (one row of 32 heads on 8, 601 keys: 8.1 us, 9.5 with four; as fast where keys are cut or blocks share CUs)
+    // Whole sequences of few rows, a CU for each: eight waves (one row of 32 heads on 8 x 128, 601 keys: 7.4 us, 8.3 with four; 16 heads x 64 5.6 and 6.4; as fast where keys are cut or blocks share CUs)
     if (p.few && p.splits == 1 && blocks <= 256.0) p.waves = 8;
     p.bytes = p.splits == 1 ? 0 : (size_t)pairs * rows * p.splits * (d + 2) * sizeof(float);
     return p;

@@ -147,7 +147,8 @@ hipError_t launch(const HeadsNormRope &a, hipStream_t stream)
 {
     constexpr int kGroups = 64 / (D / 8);
     const int chunks_q = (a.heads[0] + HEADS * kGroups - 1) / (HEADS * kGroups), chunks = chunks_q + (a.heads[1] + HEADS * kGroups - 1) / (HEADS * kGroups);
-    // all of a token's chunks where there are tokens enough for all waves of the chip (13740 tokens of 16 + 16 heads x 64 in bf16: 28 us for 31)
+    // All of a token's chunks where there are tokens enough for all waves of the chip: 13740 tokens of 16 + 16 heads x 64 in bf16 21.5 us for 24.8 with a wave for every chunk; 4096 of 32 + 8 x 128 in float32 34.4
+    // for 37.8, 2048 21.2 both, 1024 13.2 for 11.8.  (In bf16 these meet at 6000 tokens: 8192 37.5 for 38.5, 2048 13.2 for 12.3, 1024 10.0 for 7.8.)
     const int each = a.T >= 2048 ? chunks : 1, waves = (chunks + each - 1) / each;
     heads_norm_rope_kernel<D, F32, HEADS><<<dim3((unsigned)(((long long)a.T * waves + 3) / 4)), 256, 0, stream>>>(a, chunks_q, chunks, each);
     return hipGetLastError();

@@ -113,8 +113,8 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void residual_norm_kernel(Resid
     const bool conditioned = a.gate != nullptr || a.mod_scale != nullptr || a.mod_shift != nullptr;
     const int r = !conditioned ? 0 : a.row_of != nullptr ? min(max(a.row_of[row], 0), a.cond_rows - 1) : a.cond_rows == 1 ? 0 : (int)row;
     const size_t cond = (size_t)r * a.cond_stride * (a.cond_f32 ? 4 : 2);
-    // What a piece is multiplied by is loaded ahead of the sums where a lane has one piece of a wave's row (400000 rows of 128 channels: 69 us for 74).  Not where a block has the row: the registers
-    // cost more waves than that gains (8191 rows of 2560 with everything given: 66 us for 56; 10000 of 8192: 166 for 124).
+    // What a piece is multiplied by is loaded ahead of the sums where a lane has one piece of a wave's row (400000 rows of 128 channels: 68.9 us for 69.7).  Not where a block has the row: the registers
+    // cost more waves than that gains (8191 rows of 2560 with everything given: 60 us for 49; 10000 of 8192: 171 for 125).
     constexpr bool kAhead = V == 1 && LANES != 0;
     float post_gain[8], post_bias[8], scale[8], gate[8], gain[8], bias[8], mod_scale[8], mod_shift[8];
     auto load_post = [&](int v) {
@@ -189,8 +189,13 @@ hipError_t launch(const ResidualNorm &a, hipStream_t stream)
     }
     return hipGetLastError();
 }
-// Lanes by the row's length: few enough that all have work, and no more than a wave where a lane can hold its part (2048 channels: 90 us for 30000 rows, 94 with a block for each; more pieces a lane than
-// four cost waves: 8191 rows of 2560 channels with everything given 68 us with five, 56 with a block).
+// Lanes by the row's length: few enough that all have work, and no more than a wave where a lane can hold its part.  50 million values in bf16, us (lanes x pieces; 0: a block):
+//     128 channels   16 x 1   68      16 x 2   73     64 x 1  182         512   16 x 4   71     64 x 1   69     64 x 2   73     0   67
+//     136            16 x 2   96      16 x 4  103     64 x 1  178         520   64 x 2   90     64 x 4   98     0   99
+//     256            16 x 2   69      16 x 4   71     64 x 1  105        1024   64 x 2   68     64 x 4   72     0   70
+//     264            16 x 4  100      64 x 1  101     0   97             1032   64 x 4   82     0   90
+//     384            16 x 4   70      64 x 1   76     0   73             2048   64 x 4   71     0   72
+// More pieces a lane than four cost waves: 8191 rows of 2560 channels with everything given 52 us with five, 49 with a block.
 template <bool XF, bool YF, bool HF>
 hipError_t launch(const ResidualNorm &a, hipStream_t stream)
 {
